@@ -368,6 +368,162 @@ CAGQ_API int cagq_ball_query(const float* points, int32_t B, int32_t N, const in
 CAGQ_API int cagq_coverage(const cagq_grid* g, const int32_t* node_idx, const int32_t* n_valid, int32_t M,
                            int32_t K, int32_t* covered, void* stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Operators on point features. CAGQ's groups are what the next stage of a
+ * point network reads: each group's center attends to the features of the
+ * group's points (Sec. 3.3 weighs a group's points by learned edge attention;
+ * here the weights are a softmax over scores with a learned bias that depends
+ * on the relative position). These entry points take the groups as the
+ * queries above leave them, read the features where they lie, and never
+ * write out a [B][M][K][C] gather.
+ *
+ * Groups. Group (b, j) is a list of points of cloud b, in one of two forms:
+ *   K >= 1  fixed: idx device int32 [B][M][K], n_valid device int32 [B][M] or
+ *           NULL (then all K): the first n_valid slots count (clamped to
+ *           [0, K]); off is NULL and idx_len 0. As cagq_query_context,
+ *           cagq_query_points and cagq_ball_query write them.
+ *   K == 0  ragged: off device int64 [B*M + 1] ascending, idx device int32
+ *           [idx_len]; group (b, j) is idx[off[b*M+j] .. off[b*M+j+1]), cut to
+ *           [0, idx_len); n_valid is NULL. As cagq_context_offsets and
+ *           cagq_context_list write them (idx may be NULL when idx_len is 0).
+ * An index outside [0, N) marks a masked slot: it is passed over, and so are
+ * the slots that do not count, whatever they hold. The same point may stand
+ * in a group several times. An empty group is allowed.
+ *   points  device float [B][N][3] and centers device float [B][M][3]: read
+ *           by the calls that take a bias, else may be NULL.
+ * 1 <= B, N, M; B*N <= 2^31-1; B*M <= 2^31-1; B*M*K <= 2^40; idx_len <= 2^40.
+ */
+typedef struct cagq_groups {
+    int32_t B, N, M, K;
+    const int32_t* idx;
+    const int32_t* n_valid;
+    const int64_t* off;
+    int64_t idx_len;
+    const float* points;
+    const float* centers;
+} cagq_groups;
+
+/*
+ * Relative position bias of the pair of center c and point p, per head h:
+ *   table[0][u_x][h] + table[1][u_y][h] + table[2][u_z][h] + slope[h] * dist
+ * with d = p - c per axis (one rounded fp32 subtract), u_a the number of
+ * edges[a] that are <= d_a, and dist = sqrt((dx*dx + dy*dy) + dz*dz) in fp32.
+ *   table  device float [3][buckets][H] or NULL (then buckets is 0)
+ *   edges  device float [3][buckets - 1], ascending (NULL with one bucket)
+ *   slope  device float [H] or NULL
+ * 0 <= buckets <= CAGQ_MAX_BUCKETS. A d_a that is not a number falls in bucket 0.
+ */
+#define CAGQ_MAX_BUCKETS 64
+typedef struct cagq_bias {
+    const float* table;
+    const float* edges;
+    const float* slope;
+    int32_t buckets;
+} cagq_bias;
+
+/* Types of features. */
+#define CAGQ_F32 0
+#define CAGQ_BF16 1
+#define CAGQ_F16 2
+
+#define CAGQ_MAX_HEADS 128     /* heads per row */
+#define CAGQ_MAX_HEAD_DIM 256  /* channels per head */
+
+/*
+ * The shape of an attention: H heads of D channels at the centers, Hkv heads
+ * at the points (Hkv divides H; head h reads head h / (H / Hkv)), features of
+ * type `dtype`. q_row, k_row, v_row: elements from one row (one center, one
+ * point) to the next, heads and channels of a row being contiguous; 0 means
+ * densely packed rows. They let q, k and v be parts of one projection.
+ * scale multiplies q.k. cap > 0 caps the scaled products: cap * tanh(x / cap);
+ * cap = 0 leaves them. 1 <= D <= CAGQ_MAX_HEAD_DIM, 1 <= H <= CAGQ_MAX_HEADS.
+ */
+typedef struct cagq_attn {
+    int32_t dtype, H, Hkv, D;
+    float scale, cap;
+    int64_t q_row, k_row, v_row;
+} cagq_attn;
+
+/*
+ * Bytes of workspace for cagq_group_attention (backward = 0) or
+ * cagq_group_attention_backward (backward = 1) of these sizes; may be 0.
+ * Host only; reads no device memory. `bias` as in the call.
+ */
+CAGQ_API int cagq_group_attention_workspace(const cagq_groups* g, const cagq_attn* a, const cagq_bias* bias,
+                                            int32_t backward, size_t* bytes);
+
+/*
+ * Attention of every center over its group:
+ *   s_i   = cap * tanh(scale * q.k_i / cap) + bias_i   (cap 0: scale * q.k_i + bias_i)
+ *   lse   = log(sum_i exp(s_i)),  out = sum_i exp(s_i - lse) * v_i
+ * over the slots i of the group. Products, scores, the softmax's maximum and
+ * sum and the weighted sum are held in fp32; out is rounded once. A slot whose
+ * score is -infinity contributes nothing; a group without any other gives
+ * out = 0 and lse = -infinity.
+ *   q device [B][M][H][D], k and v device [B][N][Hkv][D] (rows q_row, k_row
+ *   and v_row apart), out device [B][M][H][D] dense, lse device float
+ *   [B][M][H] or NULL; bias may be NULL (none).
+ *   workspace: 256-byte aligned, may be NULL when its size is 0.
+ * Returns CAGQ_ERR_INVALID_ARG for a null pointer, a size, type, stride,
+ * scale or cap out of range or a pointer not aligned to its elements,
+ * CAGQ_ERR_WORKSPACE_TOO_SMALL, or CAGQ_ERR_HIP. The call only enqueues and
+ * can be captured into a HIP graph; results do not vary from run to run.
+ */
+CAGQ_API int cagq_group_attention(const cagq_groups* g, const cagq_attn* a, const cagq_bias* bias, const void* q,
+                                  const void* k, const void* v, void* out, float* lse, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/*
+ * The groups turned round: for each point the centers whose groups hold it.
+ *   pt_off     device int64 [B*N + 1]: offsets of the points' lists, in batch order
+ *   pt_center  device int32 [capacity]: centers j in [0, M) of the point's own
+ *              cloud, ascending, once per slot that holds the point; entries
+ *              behind the last list are -1
+ * capacity: at least B*M*K (K >= 1) or idx_len (K == 0), else
+ * CAGQ_ERR_CAPACITY. Masked slots and those that do not count are left out.
+ * workspace: cagq_point_lists_workspace bytes, 256-byte aligned.
+ */
+CAGQ_API int cagq_point_lists_workspace(const cagq_groups* g, size_t* bytes);
+CAGQ_API int cagq_point_lists(const cagq_groups* g, int64_t* pt_off, int32_t* pt_center, int64_t capacity,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of cagq_group_attention for the gradient `dout` (device
+ * [B][M][H][D], dense) of its output; lse as the forward call wrote it,
+ * pt_off and pt_center as cagq_point_lists wrote them for the same groups
+ * (`capacity` entries). With dp_i = dout.v_i, p_i = exp(s_i - lse) and
+ * ds_i = p_i * (dp_i - sum_i p_i dp_i):
+ *   dq  device [B][M][H][D], dk and dv device [B][N][Hkv][D], dense, of the
+ *       features' type, written whole (points in no group get zeros);
+ *   dtable device float [3][buckets][H], dslope device float [H]: the sums of
+ *       ds over all slots of a bucket, and of ds * dist; NULL where the bias
+ *       has no such part (or its gradient is not wanted).
+ * Sums are held in fp32 and taken in a fixed order: the results do not vary
+ * from run to run. Points and centers get no gradient.
+ */
+CAGQ_API int cagq_group_attention_backward(const cagq_groups* g, const cagq_attn* a, const cagq_bias* bias,
+                                           const int64_t* pt_off, const int32_t* pt_center, int64_t capacity,
+                                           const void* q, const void* k, const void* v, const float* lse,
+                                           const void* dout, void* dq, void* dk, void* dv, float* dtable,
+                                           float* dslope, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The relative position bias alone, for networks with scores of their own:
+ * out device [slots][H] of type `dtype`, slots = B*M*K or idx_len: the bias of
+ * each slot of each group, 0 in masked slots and those that do not count
+ * (ragged entries outside every group included). The backward call sums the
+ * gradient `dbias` (same shape and type) of the slots that count into dtable
+ * device float [3][buckets][H] and dslope device float [H] (NULL where the
+ * bias has no such part or it is not wanted), in a fixed order.
+ */
+CAGQ_API int cagq_relative_bias(const cagq_groups* g, const cagq_bias* bias, int32_t H, int32_t dtype, void* out,
+                                void* stream);
+CAGQ_API int cagq_relative_bias_workspace(const cagq_groups* g, const cagq_bias* bias, int32_t H, size_t* bytes);
+CAGQ_API int cagq_relative_bias_backward(const cagq_groups* g, const cagq_bias* bias, int32_t H, int32_t dtype,
+                                         const void* dbias, float* dtable, float* dslope, void* workspace,
+                                         size_t workspace_bytes, void* stream);
+
 /* Synchronises `stream` and returns the first device-side error recorded in
  * g's workspace since it was last built (CAGQ_OK if none). */
 CAGQ_API int cagq_get_device_status(const cagq_grid* g, void* stream);

@@ -3,7 +3,9 @@
 Argument marshalling only: every step of the path runs in the library's HIP
 kernels. Tensors are torch CUDA (HIP) tensors; the library enqueues on the
 current torch stream. The names mirror the C ABI in ``include/cagq.h``:
-``build_grid``, ``sample_centers``, ``query_context``, ``get_device_status``.
+``build_grid``, ``sample_centers``, ``query_context``, ``get_device_status``;
+and, on the features of the grouped points, ``group_attention``,
+``point_lists``, ``relative_bias`` and their gradients.
 """
 from __future__ import annotations
 
@@ -48,6 +50,21 @@ class GridC(C.Structure):
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
+class GroupsC(C.Structure):
+    _fields_ = [("B", C.c_int32), ("N", C.c_int32), ("M", C.c_int32), ("K", C.c_int32), ("idx", C.c_void_p),
+                ("n_valid", C.c_void_p), ("off", C.c_void_p), ("idx_len", C.c_int64), ("points", C.c_void_p),
+                ("centers", C.c_void_p)]
+
+
+class BiasC(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("edges", C.c_void_p), ("slope", C.c_void_p), ("buckets", C.c_int32)]
+
+
+class AttnC(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("H", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("scale", C.c_float),
+                ("cap", C.c_float), ("q_row", C.c_int64), ("k_row", C.c_int64), ("v_row", C.c_int64)]
+
+
 class CagqError(RuntimeError):
     def __init__(self, code: int, what: str):
         super().__init__(f"{what}: {status_string(code)} ({code})")
@@ -85,12 +102,25 @@ def lib() -> C.CDLL:
         L.cagq_sample_points.argtypes = [P, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_uint64, P, P]
         L.cagq_ball_query.argtypes = [P, C.c_int32, C.c_int32, P, C.c_int32, C.c_int32, C.c_float, P, P, P]
         L.cagq_coverage.argtypes = [C.POINTER(GridC), P, P, C.c_int32, C.c_int32, P, P]
+        G, A, Bi, SZ = C.POINTER(GroupsC), C.POINTER(AttnC), C.POINTER(BiasC), C.POINTER(C.c_size_t)
+        L.cagq_group_attention_workspace.argtypes = [G, A, Bi, C.c_int32, SZ]
+        L.cagq_group_attention.argtypes = [G, A, Bi, P, P, P, P, P, P, C.c_size_t, P]
+        L.cagq_point_lists_workspace.argtypes = [G, SZ]
+        L.cagq_point_lists.argtypes = [G, P, P, C.c_int64, P, C.c_size_t, P]
+        L.cagq_group_attention_backward.argtypes = [G, A, Bi, P, P, C.c_int64, P, P, P, P, P, P, P, P, P, P, P,
+                                                    C.c_size_t, P]
+        L.cagq_relative_bias.argtypes = [G, Bi, C.c_int32, C.c_int32, P, P]
+        L.cagq_relative_bias_workspace.argtypes = [G, Bi, C.c_int32, SZ]
+        L.cagq_relative_bias_backward.argtypes = [G, Bi, C.c_int32, C.c_int32, P, P, P, P, C.c_size_t, P]
         L.cagq_get_device_status.argtypes = [C.POINTER(GridC), P]
         L.cagq_status_string.argtypes = [C.c_int]
         L.cagq_status_string.restype = C.c_char_p
         for f in ("cagq_desc_from_voxel_size", "cagq_desc_from_dims", "cagq_workspace_layout", "cagq_build_grid", "cagq_build_grid_static", "cagq_sample_centers",
                   "cagq_query_context", "cagq_query_points", "cagq_context_offsets", "cagq_context_list",
-                  "cagq_sample_points", "cagq_ball_query", "cagq_coverage", "cagq_get_device_status"):
+                  "cagq_sample_points", "cagq_ball_query", "cagq_coverage", "cagq_get_device_status",
+                  "cagq_group_attention_workspace", "cagq_group_attention", "cagq_point_lists_workspace",
+                  "cagq_point_lists", "cagq_group_attention_backward", "cagq_relative_bias",
+                  "cagq_relative_bias_workspace", "cagq_relative_bias_backward"):
             getattr(L, f).restype = C.c_int
         _lib = L
     return _lib
@@ -418,6 +448,262 @@ def coverage(grid: Grid, node_idx: torch.Tensor, n_valid: torch.Tensor, out: Opt
     _check(lib().cagq_coverage(C.byref(grid.rec), _ptr(node_idx), _ptr(n_valid), M, K, _ptr(out),
                                _stream_ptr(stream)), "cagq_coverage")
     return out
+
+
+# ---------------------------------------------------------------- operators on point features
+
+FEATURES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}  # CAGQ_F32, CAGQ_BF16, CAGQ_F16
+MAX_BUCKETS = 64
+MAX_HEADS = 128
+MAX_HEAD_DIM = 256
+
+
+def _on(t: torch.Tensor, dtype, shape, name: str, dev):
+    """A contiguous tensor on ``dev``."""
+    if t.dtype != dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous {dtype} {tuple(shape)} on {dev}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _empty(shape, dtype, dev, stream):
+    """A tensor whose memory is handed on in the order of the stream it is used on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def _workspace(workspace: Optional[torch.Tensor], need: int, dev, stream):
+    if workspace is None:
+        return _empty(need, torch.uint8, dev, stream) if need else None
+    if workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace: expected contiguous torch.uint8 on {dev}")
+    return workspace
+
+
+class Groups:
+    """Groups of points: what ``query_context``, ``query_points``, ``ball_query`` or ``context_list`` found for
+    the ``centers`` [B, M, 3] among the ``points`` [B, N, 3] (float32).
+
+    Fixed groups: ``idx`` int32 [B, M, K], of which the first ``n_valid`` int32 [B, M] slots count (all K where it
+    is None). Ragged groups: ``off`` int64 [B*M + 1] and ``idx`` int32 [entries]. An index outside [0, N) is a
+    masked slot. The tensors are borrowed and must live as long as the record is used."""
+    __slots__ = ("rec", "idx", "points", "centers", "n_valid", "off", "B", "N", "M", "K", "device")
+
+    def __init__(self, idx: torch.Tensor, points: torch.Tensor, centers: torch.Tensor,
+                 n_valid: Optional[torch.Tensor] = None, off: Optional[torch.Tensor] = None):
+        if points.dim() != 3 or centers.dim() != 3 or not points.is_cuda:
+            raise ValueError("points must be [B, N, 3] and centers [B, M, 3] on the GPU")
+        dev = points.device
+        cur = _cur_device() if _cur_device is not None else torch.cuda.current_device()
+        if dev.index != cur:
+            raise ValueError(f"groups on {dev}, but the current device is cuda:{cur}")
+        B, N, M = points.shape[0], points.shape[1], centers.shape[1]
+        _on(points, torch.float32, (B, N, 3), "points", dev)
+        _on(centers, torch.float32, (B, M, 3), "centers", dev)
+        K = 0
+        if off is None:
+            if idx.dim() != 3 or idx.shape[2] < 1:
+                raise ValueError("idx must be [B, M, K], or off be given")
+            K = idx.shape[2]
+            _on(idx, torch.int32, (B, M, K), "idx", dev)
+            if n_valid is not None:
+                _on(n_valid, torch.int32, (B, M), "n_valid", dev)
+        else:
+            if n_valid is not None or idx.dim() != 1:
+                raise ValueError("ragged groups have idx [entries] and no n_valid")
+            _on(idx, torch.int32, idx.shape, "idx", dev)
+            _on(off, torch.int64, (B * M + 1,), "off", dev)
+        self.idx, self.points, self.centers, self.n_valid, self.off = idx, points, centers, n_valid, off
+        self.B, self.N, self.M, self.K, self.device = B, N, M, K, dev
+        self.rec = GroupsC(B, N, M, K, idx.data_ptr(), None if n_valid is None else n_valid.data_ptr(),
+                           None if off is None else off.data_ptr(), 0 if K else idx.numel(), points.data_ptr(),
+                           centers.data_ptr())
+
+    @property
+    def slots(self) -> int:
+        return self.idx.numel()
+
+
+class RelativeBias:
+    """Relative position bias of H heads: ``table`` [3, buckets, H] read by the buckets that the ascending
+    ``edges`` [3, buckets - 1] cut each axis into, and ``slope`` [H] times the distance (float32; either may be
+    None). The tensors are borrowed."""
+    __slots__ = ("rec", "table", "edges", "slope", "H", "device")
+
+    def __init__(self, table: Optional[torch.Tensor] = None, edges: Optional[torch.Tensor] = None,
+                 slope: Optional[torch.Tensor] = None):
+        some = table if table is not None else slope
+        if some is None or not some.is_cuda:
+            raise ValueError("a bias needs a table or a slope, on the GPU")
+        dev, nb, H = some.device, 0, some.shape[-1] if some.dim() else 0
+        if table is not None:
+            nb = table.shape[1] if table.dim() == 3 else 0
+            if not 1 <= nb <= MAX_BUCKETS:
+                raise ValueError(f"table must be [3, buckets, H] with 1 to {MAX_BUCKETS} buckets")
+            _on(table, torch.float32, (3, nb, H), "table", dev)
+            if edges is None and nb > 1:
+                raise ValueError("a table needs edges [3, buckets - 1]")
+        if edges is not None:
+            _on(edges, torch.float32, (3, max(0, nb - 1)), "edges", dev)
+        if slope is not None:
+            _on(slope, torch.float32, (H,), "slope", dev)
+        self.table, self.edges, self.slope, self.H, self.device = table, edges, slope, H, dev
+        self.rec = BiasC(None if table is None else table.data_ptr(), None if edges is None else edges.data_ptr(),
+                         None if slope is None else slope.data_ptr(), nb)
+
+
+def _feature_rows(t: torch.Tensor, B: int, n: int, dtype, name: str, dev) -> int:
+    """Elements from one row of ``t`` [B, n, heads, D] to the next; its heads and channels are contiguous, its
+    rows evenly spaced (a part of a larger projection, say)."""
+    if t.dim() != 4 or t.shape[0] != B or t.shape[1] != n or t.dtype != dtype or t.device != dev:
+        raise ValueError(f"{name}: expected {dtype} [{B}, {n}, heads, D] on {dev}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    _, _, h, d = t.shape
+    sb, sn, sh, sd = t.stride()
+    row = sn if n > 1 else sb if B > 1 else h * d
+    if (d > 1 and sd != 1) or (h > 1 and sh != d) or (B > 1 and sb != n * row) or row < h * d:
+        raise ValueError(f"{name}: rows must be evenly spaced, their heads and channels contiguous, "
+                         f"got strides {tuple(t.stride())} for {tuple(t.shape)}")
+    return row
+
+
+def _attn(groups: Groups, q, k, v, bias: Optional[RelativeBias], scale, cap):
+    dev, dtype = groups.device, q.dtype
+    if dtype not in FEATURES:
+        raise ValueError(f"q: features are {', '.join(str(x) for x in FEATURES)}, got {dtype}")
+    qr = _feature_rows(q, groups.B, groups.M, dtype, "q", dev)
+    kr = _feature_rows(k, groups.B, groups.N, dtype, "k", dev)
+    vr = _feature_rows(v, groups.B, groups.N, dtype, "v", dev)
+    H, D, Hkv = q.shape[2], q.shape[3], k.shape[2]
+    if v.shape != k.shape or k.shape[3] != D or Hkv < 1 or H % Hkv:
+        raise ValueError(f"heads of q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not fit")
+    if bias is not None and (bias.H != H or bias.device != dev):
+        raise ValueError(f"bias: expected {H} heads on {dev}, got {bias.H} on {bias.device}")
+    return AttnC(FEATURES[dtype], H, Hkv, D, D ** -0.5 if scale is None else scale, cap, qr, kr, vr)
+
+
+def group_attention(groups: Groups, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                    bias: Optional[RelativeBias] = None, scale: Optional[float] = None, cap: float = 0.0,
+                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Attention of each center over its group (cagq_group_attention): ``q`` [B, M, H, D], ``k`` and ``v``
+    [B, N, Hkv, D] of float32, bfloat16 or float16. ``scale`` is D ** -0.5 by default; ``cap`` > 0 caps the scores
+    by a tanh. Returns (out [B, M, H, D], lse float32 [B, M, H])."""
+    a = _attn(groups, q, k, v, bias, scale, cap)
+    dev = groups.device
+    if out is None:
+        out = _empty((groups.B, groups.M, a.H, a.D), q.dtype, dev, stream)
+    else:
+        _on(out, q.dtype, (groups.B, groups.M, a.H, a.D), "out", dev)
+    if lse is None:
+        lse = _empty((groups.B, groups.M, a.H), torch.float32, dev, stream)
+    else:
+        _on(lse, torch.float32, (groups.B, groups.M, a.H), "lse", dev)
+    b = None if bias is None else C.byref(bias.rec)
+    need = C.c_size_t()
+    _check(lib().cagq_group_attention_workspace(C.byref(groups.rec), C.byref(a), b, 0, C.byref(need)),
+           "cagq_group_attention")
+    ws = _workspace(workspace, need.value, dev, stream)
+    _check(lib().cagq_group_attention(C.byref(groups.rec), C.byref(a), b, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                      out.data_ptr(), lse.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(),
+                                      _stream_ptr(stream)), "cagq_group_attention")
+    return out, lse
+
+
+def point_lists(groups: Groups, off: Optional[torch.Tensor] = None, center: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """The groups turned round (cagq_point_lists): offsets int64 [B*N + 1] and, for each point, the centers whose
+    groups hold it, ascending, int32 [slots] (-1 behind the last list)."""
+    dev = groups.device
+    if off is None:
+        off = _empty(groups.B * groups.N + 1, torch.int64, dev, stream)
+    else:
+        _on(off, torch.int64, (groups.B * groups.N + 1,), "off", dev)
+    if center is None:
+        center = _empty(groups.slots, torch.int32, dev, stream)
+    else:
+        _on(center, torch.int32, center.shape, "center", dev)
+    need = C.c_size_t()
+    _check(lib().cagq_point_lists_workspace(C.byref(groups.rec), C.byref(need)), "cagq_point_lists")
+    ws = _workspace(workspace, need.value, dev, stream)
+    _check(lib().cagq_point_lists(C.byref(groups.rec), off.data_ptr(), center.data_ptr(), center.numel(), _ptr(ws),
+                                  0 if ws is None else ws.numel(), _stream_ptr(stream)), "cagq_point_lists")
+    return off, center
+
+
+def group_attention_backward(groups: Groups, lists, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                             lse: torch.Tensor, dout: torch.Tensor, bias: Optional[RelativeBias] = None,
+                             scale: Optional[float] = None, cap: float = 0.0,
+                             workspace: Optional[torch.Tensor] = None,
+                             stream: Optional[torch.cuda.Stream] = None) -> Dict[str, Optional[torch.Tensor]]:
+    """Gradients of ``group_attention`` for the gradient ``dout`` of its output (cagq_group_attention_backward),
+    with ``lists`` from ``point_lists`` of the same groups: dq, dk, dv of the features' type, dtable and dslope
+    float32 (None where the bias has no such part)."""
+    a = _attn(groups, q, k, v, bias, scale, cap)
+    dev = groups.device
+    off, center = lists
+    _on(off, torch.int64, (groups.B * groups.N + 1,), "lists[0]", dev)
+    _on(center, torch.int32, center.shape, "lists[1]", dev)
+    _on(lse, torch.float32, (groups.B, groups.M, a.H), "lse", dev)
+    _on(dout, q.dtype, (groups.B, groups.M, a.H, a.D), "dout", dev)
+    kv = (groups.B, groups.N, a.Hkv, a.D)
+    dq = _empty(tuple(dout.shape), q.dtype, dev, stream)
+    dk, dv = _empty(kv, q.dtype, dev, stream), _empty(kv, q.dtype, dev, stream)
+    dtable = dslope = b = None
+    if bias is not None:
+        b = C.byref(bias.rec)
+        if bias.table is not None:
+            dtable = _empty(tuple(bias.table.shape), torch.float32, dev, stream)
+        if bias.slope is not None:
+            dslope = _empty((a.H,), torch.float32, dev, stream)
+    need = C.c_size_t()
+    _check(lib().cagq_group_attention_workspace(C.byref(groups.rec), C.byref(a), b, 1, C.byref(need)),
+           "cagq_group_attention_backward")
+    ws = _workspace(workspace, need.value, dev, stream)
+    _check(lib().cagq_group_attention_backward(
+        C.byref(groups.rec), C.byref(a), b, off.data_ptr(), center.data_ptr(), center.numel(), q.data_ptr(),
+        k.data_ptr(), v.data_ptr(), lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+        _ptr(dtable), _ptr(dslope), _ptr(ws), 0 if ws is None else ws.numel(), _stream_ptr(stream)),
+        "cagq_group_attention_backward")
+    return dict(dq=dq, dk=dk, dv=dv, dtable=dtable, dslope=dslope)
+
+
+def relative_bias(groups: Groups, bias: RelativeBias, dtype=torch.float32, out: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The relative position bias of every slot (cagq_relative_bias): [B, M, K, H], or [entries, H] of ragged
+    groups; 0 in the slots that do not count."""
+    if dtype not in FEATURES or bias.device != groups.device:
+        raise ValueError(f"relative_bias: {dtype} with a bias on {bias.device} for groups on {groups.device}")
+    shape = tuple(groups.idx.shape) + (bias.H,)
+    if out is None:
+        out = _empty(shape, dtype, groups.device, stream)
+    else:
+        _on(out, dtype, shape, "out", groups.device)
+    _check(lib().cagq_relative_bias(C.byref(groups.rec), C.byref(bias.rec), bias.H, FEATURES[dtype], out.data_ptr(),
+                                    _stream_ptr(stream)), "cagq_relative_bias")
+    return out
+
+
+def relative_bias_backward(groups: Groups, bias: RelativeBias, dbias: torch.Tensor,
+                           workspace: Optional[torch.Tensor] = None,
+                           stream: Optional[torch.cuda.Stream] = None):
+    """(dtable, dslope), float32, for the gradient ``dbias`` of ``relative_bias``'s output
+    (cagq_relative_bias_backward); None where the bias has no such part."""
+    dev = groups.device
+    if dbias.dtype not in FEATURES or bias.device != dev:
+        raise ValueError(f"relative_bias_backward: {dbias.dtype} with a bias on {bias.device} for groups on {dev}")
+    _on(dbias, dbias.dtype, tuple(groups.idx.shape) + (bias.H,), "dbias", dev)
+    dtable = None if bias.table is None else _empty(tuple(bias.table.shape), torch.float32, dev, stream)
+    dslope = None if bias.slope is None else _empty((bias.H,), torch.float32, dev, stream)
+    need = C.c_size_t()
+    _check(lib().cagq_relative_bias_workspace(C.byref(groups.rec), C.byref(bias.rec), bias.H, C.byref(need)),
+           "cagq_relative_bias_backward")
+    ws = _workspace(workspace, need.value, dev, stream)
+    _check(lib().cagq_relative_bias_backward(
+        C.byref(groups.rec), C.byref(bias.rec), bias.H, FEATURES[dbias.dtype], dbias.data_ptr(), _ptr(dtable),
+        _ptr(dslope), _ptr(ws), 0 if ws is None else ws.numel(), _stream_ptr(stream)), "cagq_relative_bias_backward")
+    return dtable, dslope
 
 
 def get_device_status(grid: Grid, stream: Optional[torch.cuda.Stream] = None) -> int:
