@@ -8,6 +8,7 @@ namespace {
 
 constexpr int kRbThreads = 256;
 constexpr int kRbWaves = kRbThreads / kWave;
+constexpr int kRedThreads = 1024;
 constexpr int kRbParts = 1024;   // workgroups of the gradient, each with partial sums of its own
 constexpr int kRbLds = 128 << 10;  // LDS of their tables, a table per wave
 
@@ -15,7 +16,7 @@ constexpr int kRbLds = 128 << 10;  // LDS of their tables, a table per wave
 // wave's, 64 slots at a time. f(first slot, number of slots, row, u, dist,
 // counts) with the lane's own slot's row, place and whether it counts.
 template <typename F>
-__device__ __forceinline__ void each_chunk(const Groups& g, const Bias& b, F f) {
+__device__ __forceinline__ void each_chunk(const Groups& g, const Bias& b, const Edges& ed, F f) {
     const int lane = lane_id();
     const int waves_b = blockDim.x / kWave;
     const int64_t waves = (int64_t)gridDim.x * waves_b;
@@ -30,7 +31,7 @@ __device__ __forceinline__ void each_chunk(const Groups& g, const Bias& b, F f) 
                 float p[3], c[3];
                 load_xyz(g.points, (int64_t)udiv((uint32_t)row, g.mm) * g.N + i, p);
                 load_xyz(g.centers, row, c);
-                pair_place(b.edges, b.nb, b.slope != nullptr, p, c, u, dist);
+                pair_place(ed, b.slope != nullptr, p, c, u, dist);
             }
         }
         f(s0, n, u, dist, counts);
@@ -58,8 +59,11 @@ __device__ __forceinline__ void each_chunk(const Groups& g, const Bias& b, F f) 
 
 template <typename T>
 __global__ __launch_bounds__(kRbThreads) void k_rb(Groups g, Bias b, T* __restrict__ out) {
+    __shared__ float s_edges[3 * (CAGQ_MAX_BUCKETS - 1)];
     const int lane = lane_id();
-    each_chunk(g, b, [&](int64_t s0, int n, uint32_t u, float dist, bool counts) {
+    const Edges ed = stage_edges(b, s_edges);
+    __syncthreads();
+    each_chunk(g, b, ed, [&](int64_t s0, int n, uint32_t u, float dist, bool counts) {
         const uint64_t live = __ballot(counts);
         for (int e = lane; e < ((n * b.H + kWave - 1) & -kWave); e += kWave) {
             const int p = e / b.H, h = e - p * b.H;
@@ -91,13 +95,15 @@ template <typename T>
 __global__ __launch_bounds__(kRbThreads) void k_rb_back(Groups g, Bias b, const T* __restrict__ dbias,
                                                         float* __restrict__ part) {
     extern __shared__ float s_tab[];
+    __shared__ float s_edges[3 * (CAGQ_MAX_BUCKETS - 1)];
     const int lane = lane_id();
+    const Edges ed = stage_edges(b, s_edges);
     const int entries = (3 * b.nb + 1) * b.H;
     const int waves_b = blockDim.x / kWave;
     for (int e = threadIdx.x; e < entries * waves_b; e += blockDim.x) s_tab[e] = 0.0f;
     __syncthreads();
     float* tab = s_tab + (threadIdx.x / kWave) * entries;
-    each_chunk(g, b, [&](int64_t s0, int n, uint32_t u, float dist, bool counts) {
+    each_chunk(g, b, ed, [&](int64_t s0, int n, uint32_t u, float dist, bool counts) {
         const uint64_t live = __ballot(counts);
         for (int e = lane; e < ((n * b.H + kWave - 1) & -kWave); e += kWave) {
             const int p = e / b.H, h = e - p * b.H;
@@ -121,20 +127,32 @@ __global__ __launch_bounds__(kRbThreads) void k_rb_back(Groups g, Bias b, const 
     }
 }
 
-__global__ __launch_bounds__(kRbThreads) void k_bias_reduce(const float* __restrict__ part, int32_t parts, int entries,
-                                                            int tab, float* __restrict__ dtable,
-                                                            float* __restrict__ dslope) {
-    const int e = blockIdx.x * (kRbThreads / kWave) + threadIdx.x / kWave, lane = lane_id();
-    if (e >= entries) return;
-    float x = 0.0f;
-    for (int p = lane; p < parts; p += kWave) x += part[(int64_t)p * entries + e];
-    x = group_sum(x, kWave);
-    if (lane == 0) {
-        if (e < tab) {
-            if (dtable) dtable[e] = x;
-        } else if (dslope) {
-            dslope[e - tab] = x;
+// Waves of a workgroup take the parts in turn, their lanes 64 entries in a row.
+__global__ __launch_bounds__(kRedThreads) void k_bias_reduce(const float* __restrict__ part, int32_t parts,
+                                                             int entries, int tab, float* __restrict__ dtable,
+                                                             float* __restrict__ dslope) {
+    constexpr int kWaves = kRedThreads / kWave;
+    __shared__ float s[kWaves][kWave];
+    const int lane = lane_id(), w = threadIdx.x / kWave;
+    const int e = blockIdx.x * kWave + lane;
+    float x[4] = {};
+    if (e < entries) {
+        int p = w;
+        for (; p + 3 * kWaves < parts; p += 4 * kWaves) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] += part[(int64_t)(p + i * kWaves) * entries + e];
         }
+        for (; p < parts; p += kWaves) x[0] += part[(int64_t)p * entries + e];
+    }
+    s[w][lane] = (x[0] + x[1]) + (x[2] + x[3]);
+    __syncthreads();
+    if (w > 0 || e >= entries) return;
+    float sum = 0.0f;
+    for (int i = 0; i < kWaves; ++i) sum += s[i][lane];
+    if (e < tab) {
+        if (dtable) dtable[e] = sum;
+    } else if (dslope) {
+        dslope[e - tab] = sum;
     }
 }
 
@@ -181,9 +199,8 @@ hipError_t rb_backward(const Groups& g, const Bias& b, const void* dbias, float*
 hipError_t launch_bias_reduce(const float* part, int32_t parts, const Bias& b, float* dtable, float* dslope,
                               hipStream_t s) {
     const int entries = (3 * b.nb + 1) * b.H;
-    const int per = kRbThreads / kWave;
-    k_bias_reduce<<<(entries + per - 1) / per, kRbThreads, 0, s>>>(part, parts, entries, 3 * b.nb * b.H, dtable,
-                                                                   b.slope ? dslope : nullptr);
+    k_bias_reduce<<<(entries + kWave - 1) / kWave, kRedThreads, 0, s>>>(part, parts, entries, 3 * b.nb * b.H, dtable,
+                                                                        b.slope ? dslope : nullptr);
     return hipGetLastError();
 }
 

@@ -65,28 +65,65 @@ __device__ __forceinline__ float to_float(bf16 x) {
     return __uint_as_float((uint32_t)__builtin_bit_cast(uint16_t, x) << 16);
 }
 
+// The 16 bytes of a lane's channels as they are stored, so that products of
+// bfloat16 can be taken two at a time.
+typedef u32x4 Raw;
+
 // n channels (of kVec) at p; the others are 0. VEC: p is 16-byte aligned and
 // all kVec channels are there (or none is wanted, n = 0).
 template <typename T, bool VEC>
-__device__ __forceinline__ void load_channels(const T* p, int n, float (&x)[kVec<T>]) {
-    constexpr int W = kVec<T>;
+__device__ __forceinline__ Raw load_channels(const T* p, int n) {
+    Raw r = {0, 0, 0, 0};
     if constexpr (VEC) {
-        u32x4 r = {0, 0, 0, 0};
         if (n > 0) r = *reinterpret_cast<const u32x4*>(p);
-        if constexpr (sizeof(T) == 4) {
+    } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(r[i]);
-        } else {
+        for (int i = 0; i < 4; ++i)
+            if (i < n) r[i] = __builtin_bit_cast(uint32_t, p[i]);
+    } else {
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[2 * i] = to_float(__builtin_bit_cast(T, (uint16_t)(r[i] & 0xFFFFu)));
-                x[2 * i + 1] = to_float(__builtin_bit_cast(T, (uint16_t)(r[i] >> 16)));
-            }
-        }
+        for (int i = 0; i < 8; ++i)
+            if (i < n) r[i / 2] |= (uint32_t)h[i] << (16 * (i & 1));
+    }
+    return r;
+}
+
+// Channel i (known at compile time) as a float.
+template <typename T>
+__device__ __forceinline__ float channel(const Raw& r, int i) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(r[i]);
+    else if constexpr (__is_same(T, bf16))
+        return __uint_as_float(i & 1 ? r[i / 2] & 0xFFFF0000u : r[i / 2] << 16);
+    else
+        return (float)__builtin_bit_cast(f16, (uint16_t)(i & 1 ? r[i / 2] >> 16 : r[i / 2] & 0xFFFFu));
+}
+
+// The lane's part of a product of two heads. bfloat16: two products and the
+// sum in one instruction (v_dot2_f32_bf16, within 2^-24 of the products'
+// magnitudes on subnormal inputs too). float16: one by one, mixed with fp32
+// (v_dot2_f32_f16 was off by 35 * 2^-24 with subnormal inputs).
+template <typename T>
+__device__ __forceinline__ float dot(const Raw& a, const Raw& b) {
+    float s = 0.0f;
+    if constexpr (__is_same(T, bf16)) {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)a[i]),
+                                                __builtin_bit_cast(bf16x2, (uint32_t)b[i]), s, false);
     } else {
 #pragma unroll
-        for (int i = 0; i < W; ++i) x[i] = i < n ? to_float(p[i]) : 0.0f;
+        for (int i = 0; i < kVec<T>; ++i) s = fmaf(channel<T>(a, i), channel<T>(b, i), s);
     }
+    return s;
+}
+
+// acc += w * channels
+template <typename T>
+__device__ __forceinline__ void add_channels(float (&acc)[kVec<T>], float w, const Raw& r) {
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) acc[i] = fmaf(w, channel<T>(r, i), acc[i]);
 }
 
 // The one rounding to the features' type, to nearest even.
@@ -113,46 +150,86 @@ __device__ __forceinline__ void store_channels(T* p, int n, const float (&x)[kVe
     }
 }
 
-__device__ __forceinline__ float xlane_f(float v, int j) { return __uint_as_float(xlane(__float_as_uint(v), j)); }
+// ------------------------------------------------------------------ lanes
 
-// Sum over groups of G lanes (a power of two, the same for the launch), in
-// every lane of the group.
-__device__ __forceinline__ float group_sum(float v, int G) {
-    if (G > 1) v += xlane_f(v, 1);
-    if (G > 2) v += xlane_f(v, 2);
-    if (G > 4) v += xlane_f(v, 4);
-    if (G > 8) v += xlane_f(v, 8);
-    if (G > 16) v += xlane_f(v, 16);
-    if (G > 32) v += xlane_f(v, 32);
-    return v;
+// Sums over groups of G lanes (a power of two, the same for the launch), in
+// every lane of the group; every lane of the wave must be active. After the
+// first steps the lanes of a quad, then of eight, hold the same value, so that
+// a mirrored row serves as the exchange at distance 4 and 8.
+template <int C>
+__device__ __forceinline__ float dpp_f(float v) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), C, 0xF, 0xF, true));
+}
+template <int N>
+__device__ __forceinline__ void group_sums(float (&v)[N], int G) {
+    if (G > 1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += dpp_f<0xB1>(v[i]);  // quad_perm 1,0,3,2
+    }
+    if (G > 2) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += dpp_f<0x4E>(v[i]);  // quad_perm 2,3,0,1
+    }
+    if (G > 4) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += dpp_f<0x141>(v[i]);  // row_half_mirror
+    }
+    if (G > 8) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += dpp_f<0x140>(v[i]);  // row_mirror
+    }
+    if (G > 16) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __uint_as_float(xlane(__float_as_uint(v[i]), 16));
+    }
+    if (G > 32) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __uint_as_float(xlane(__float_as_uint(v[i]), 32));
+    }
 }
 
 // ------------------------------------------------------------------ the bias of a pair
 
-// Number of the n ascending edges that are <= d (n < CAGQ_MAX_BUCKETS).
-__device__ __forceinline__ uint32_t bucket_of(const float* edges, int n, float d) {
-    uint32_t u = 0;
-#pragma unroll
-    for (int s = CAGQ_MAX_BUCKETS / 2; s > 0; s >>= 1)
-        if ((int)u + s <= n && edges[u + s - 1] <= d) u += s;
-    return u;
+// The edges in LDS, each axis's filled up to one less than a power of two by
+// values no distance reaches (NaN), and the steps of a search among them.
+struct Edges {
+    const float* at;  // [3][size]
+    int size;         // 2^k - 1 >= nb - 1
+};
+
+inline __host__ __device__ int edges_size(int nb) {
+    int n = 1;
+    while (n < nb) n <<= 1;
+    return n - 1;
 }
 
-// Where a pair lies: its buckets on the axes, a byte each, and its distance.
-// `edges`: [3][nb - 1], global memory or LDS.
-__device__ __forceinline__ void pair_place(const float* edges, int nb, bool want_dist, const float (&p)[3],
-                                           const float (&c)[3], uint32_t& u, float& dist) {
-    const float dx = p[0] - c[0], dy = p[1] - c[1], dz = p[2] - c[2];
-    u = 0;
-    dist = 0.0f;
-    if (nb > 1) {
-        const int n = nb - 1;
-        u = bucket_of(edges, n, dx) | bucket_of(edges + n, n, dy) << 8 | bucket_of(edges + 2 * n, n, dz) << 16;
+// Copies them (every thread of the block; the caller synchronises).
+__device__ __forceinline__ Edges stage_edges(const Bias& b, float* lds) {
+    const int size = edges_size(b.nb), n = b.nb - 1;
+    for (int e = threadIdx.x; e < 3 * size; e += blockDim.x) {
+        const int axis = e / size, k = e - axis * size;
+        lds[e] = k < n ? b.edges[axis * n + k] : __builtin_nanf("");
     }
-    if (want_dist) dist = sqrtf((dx * dx + dy * dy) + dz * dz);
+    return Edges{lds, size};
 }
 
-// Bias of head h at a place. `table`: [3][nb][H], global memory or LDS.
+// Where a pair lies: the number of edges <= d on each axis, a byte each, and
+// its distance. The three searches' steps are read together.
+__device__ __forceinline__ void pair_place(const Edges& ed, bool want_dist, const float (&p)[3], const float (&c)[3],
+                                           uint32_t& u, float& dist) {
+    const float dx = p[0] - c[0], dy = p[1] - c[1], dz = p[2] - c[2];
+    int x = 0, y = 0, z = 0;
+    for (int s = (ed.size + 1) >> 1; s > 0; s >>= 1) {
+        const float ex = ed.at[x + s - 1], ey = ed.at[ed.size + y + s - 1], ez = ed.at[2 * ed.size + z + s - 1];
+        x += ex <= dx ? s : 0;
+        y += ey <= dy ? s : 0;
+        z += ez <= dz ? s : 0;
+    }
+    u = (uint32_t)x | (uint32_t)y << 8 | (uint32_t)z << 16;
+    dist = want_dist ? sqrtf((dx * dx + dy * dy) + dz * dz) : 0.0f;
+}
+
+// Bias of head h at a place. `table`: [3][nb][H].
 __device__ __forceinline__ float bias_at(const float* table, int nb, int H, float slope, int h, uint32_t u,
                                          float dist) {
     float b = 0.0f;
@@ -204,8 +281,8 @@ struct Attn {
 };
 
 size_t group_attention_bytes(const Groups& g, int32_t B, const Attn& a, int32_t dtype, const Bias& b, bool backward);
-hipError_t launch_group_attention(const Groups& g, const Attn& a, int32_t dtype, const Bias& b, void* out, float* lse,
-                                  void* ws, hipStream_t s);
+hipError_t launch_group_attention(const Groups& g, int32_t B, const Attn& a, int32_t dtype, const Bias& b, void* out,
+                                  float* lse, void* ws, hipStream_t s);
 hipError_t launch_group_attention_backward(const Groups& g, int32_t B, const Attn& a, int32_t dtype, const Bias& b,
                                            const int64_t* pt_off, const int32_t* pt_center, int64_t capacity,
                                            const float* lse, const void* dout, void* dq, void* dk, void* dv,

@@ -126,7 +126,7 @@ int cagq_group_attention(const cagq_groups* g, const cagq_attn* a, const cagq_bi
     at.v = v;
     const int rc = check_workspace(workspace, workspace_bytes, group_attention_bytes(gr, g->B, at, a->dtype, b, false));
     if (rc != CAGQ_OK) return rc;
-    return hip_status(launch_group_attention(gr, at, a->dtype, b, out, lse, workspace, (hipStream_t)stream));
+    return hip_status(launch_group_attention(gr, g->B, at, a->dtype, b, out, lse, workspace, (hipStream_t)stream));
 }
 
 int cagq_point_lists_workspace(const cagq_groups* g, size_t* bytes) {
