@@ -8,9 +8,9 @@
 // keep many gathered rows in flight:
 //   - G lanes to a head of a row (16 bytes of features each), the row's heads
 //     side by side, and as many rows at once as the wave has lanes for (slots);
-//   - a list's indices, offsets and places in the bias are made a chunk at a
-//     time, one entry per lane, and handed to the rows' lanes by permutes;
-//   - kUnroll rows of each slot are loaded before the first is used. Loads go
+//   - a list's entries are made ready a chunk at a time, one per lane (index,
+//     place, the bias of every head), and left in LDS for the rows' lanes;
+//   - two to four rows of each slot are loaded before the first is used. Loads go
 //     through a bounds-checked buffer, in which an entry that is not there has
 //     an offset past the end and reads as zeros, without a branch;
 //   - two ways to share a wave: EACH, a list per slot (many short lists: no
@@ -37,7 +37,9 @@ constexpr int kAtThreads = 256;
 constexpr int kAtWaves = kAtThreads / kWave;
 constexpr int kAtBlocks = 256 * 8;   // workgroups of a launch; they go round where there is more to do
 constexpr int kAtParts = 1024;       // workgroups of the gradient at the points, where the bias wants its own
-constexpr int kAtLds = 144 << 10;    // LDS of a workgroup: edges, table, and the waves' gradient tables
+constexpr int kAtLds = 144 << 10;    // LDS of a workgroup: edges, table, chunks, and the waves' gradient tables
+constexpr int kTableFloats = 8192;   // largest table that a workgroup copies to LDS
+constexpr int kPoints = 16;          // most points in a row whose lists one slot walks (FLAT)
 constexpr int kJoinFloats = 2048;    // H * D up to which a workgroup's waves join their parts in LDS
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -120,26 +122,40 @@ struct Rows {
 // What all kernels know of the scores.
 struct Score {
     Edges ed;
-    const float* table;  // LDS, [3][nb][H]
+    const float* table;  // [3][nb][H], the caller's
+    const float* lds;    // a copy of it in LDS (lds_table: it takes at most kTableFloats)
+    const float* slope;  // [H], LDS (zeros where there is none)
     int nb, H;
-    bool dist;
+    bool dist, lds_table;
     float mul;   // of a product: scale, or with a cap 2 log2 e scale / cap
     float cap;
 
-    // Floats of LDS before the kernel's own.
-    static __host__ __device__ int floats(const Bias& b) { return 3 * edges_size(b.nb) + 3 * b.nb * b.H; }
+    // Floats of LDS before the kernel's own (a multiple of 4).
+    static __host__ __device__ int floats(const Bias& b) {
+        if (b.nb == 0 && !b.slope) return 0;
+        const int t = 3 * b.nb * b.H;
+        return ((t <= kTableFloats ? t : 0) + b.H + 3 * edges_size(b.nb) + 3) & ~3;
+    }
 
     // Every thread of the block; ends with a barrier.
-    __device__ __forceinline__ Score(const Bias& b, const Attn& a, float* lds) {
-        ed = stage_edges(b, lds);
-        float* t = lds + 3 * ed.size;
-        for (int e = threadIdx.x; e < 3 * b.nb * b.H; e += blockDim.x) t[e] = b.table[e];
-        table = t;
+    __device__ __forceinline__ Score(const Bias& b, const Attn& a, float* s) {
         nb = b.nb;
         H = b.H;
         dist = b.slope != nullptr;
         cap = a.cap;
         mul = cap > 0.0f ? 2.0f * kLog2e * a.scale / cap : a.scale;
+        const int t = 3 * nb * H;
+        lds_table = t <= kTableFloats;
+        table = b.table;
+        lds = s;
+        if (!placed()) return;
+        if (lds_table) {
+            for (int e = threadIdx.x; e < t; e += blockDim.x) s[e] = b.table[e];
+            s += t;
+        }
+        slope = s;
+        for (int e = threadIdx.x; e < H; e += blockDim.x) s[e] = b.slope ? b.slope[e] : 0.0f;
+        ed = stage_edges(b, s + H);
         __syncthreads();
     }
     __device__ __forceinline__ bool placed() const { return nb > 0 || dist; }
@@ -157,9 +173,6 @@ struct Score {
     }
     // 1 - tanh^2
     __device__ __forceinline__ float slack(float e) const { return cap > 0.0f ? 4.0f * e * (1.0f - e) : 1.0f; }
-    __device__ __forceinline__ float bias(int h, uint32_t u, float slope, float d) const {
-        return bias_at(table, nb, H, slope, h, u, d);
-    }
 };
 
 // exp(x) of a difference of scores.
@@ -167,6 +180,69 @@ __device__ __forceinline__ float weight(float x) { return __builtin_amdgcn_exp2f
 
 // log of a sum of weights.
 __device__ __forceinline__ float log_sum(float x) { return kLn2 * __builtin_amdgcn_logf(x); }
+
+// A chunk of a wave's entries in LDS, a row each: the bias of the wave's heads
+// (where there is a bias), then fields. The entries' lanes write the rows and
+// the slots' lanes read them; a wave's own LDS operations run in order. Rows
+// that no entry's lane writes stay without an entry. An index of kMasked is an
+// entry that is passed over, one of kNoEntry none.
+constexpr int32_t kMasked = -1, kNoEntry = -2;
+constexpr int kKey = 0, kKey2 = 1, kIndex = 2, kPlace = 3, kDist = 4, kPoint = 5, kFields = 8;
+
+struct Chunk {
+    float* rows;
+    int hp, stride;
+
+    static __host__ __device__ int floats(bool placed, int rows_n, int hp) {
+        return rows_n * ((placed ? (hp + 3) & ~3 : 0) + kFields);
+    }
+    __device__ __forceinline__ Chunk(float* lds, int rows_n, const Score& sc, int hp_) {
+        hp = sc.placed() ? (hp_ + 3) & ~3 : 0;
+        stride = hp + kFields;
+        rows = lds + (threadIdx.x / kWave) * rows_n * stride;
+        for (int r = lane_id(); r < rows_n; r += kWave) {
+            rows[r * stride + hp + kKey] = __uint_as_float(kNone);
+            rows[r * stride + hp + kKey2] = __uint_as_float(kNone);
+            rows[r * stride + hp + kIndex] = __int_as_float(kNoEntry);
+        }
+    }
+    __device__ __forceinline__ const float* row(int r) const { return rows + r * stride; }
+    __device__ __forceinline__ uint32_t field(const float* r, int f) const { return __float_as_uint(r[hp + f]); }
+
+    // The lane's entry into row r: the keys of its rows, its index (negative:
+    // none), and the bias of heads h0 .. h0 + n.
+    __device__ __forceinline__ void put(int r, uint32_t key, uint32_t key2, int32_t index, uint32_t u, float d,
+                                        const Score& sc, int h0, int n) {
+        float* o = rows + r * stride;
+        o[hp + kKey] = __uint_as_float(key);
+        o[hp + kKey2] = __uint_as_float(key2);
+        o[hp + kIndex] = __int_as_float(index);
+        if (!sc.placed()) return;
+        o[hp + kPlace] = __uint_as_float(u);
+        o[hp + kDist] = d;
+        if (index < 0) return;
+        if (((sc.H | h0 | n) & 3) == 0 && sc.lds_table) {
+            typedef float f4 __attribute__((ext_vector_type(4)));
+            const f4* t0 = (const f4*)(sc.lds + (u & 255u) * sc.H + h0);
+            const f4* t1 = (const f4*)(sc.lds + (sc.nb + (u >> 8 & 255u)) * sc.H + h0);
+            const f4* t2 = (const f4*)(sc.lds + (2 * sc.nb + (u >> 16)) * sc.H + h0);
+            for (int h = 0; h < n / 4; ++h) {
+                f4 b = d * ((const f4*)(sc.slope + h0))[h];
+                if (sc.nb > 0) b += t0[h] + t1[h] + t2[h];
+                ((f4*)o)[h] = b;
+            }
+        } else {
+            const float* t0 = sc.table + (u & 255u) * sc.H + h0;
+            const float* t1 = sc.table + (sc.nb + (u >> 8 & 255u)) * sc.H + h0;
+            const float* t2 = sc.table + (2 * sc.nb + (u >> 16)) * sc.H + h0;
+            for (int h = 0; h < n; ++h) {
+                float b = d * sc.slope[h0 + h];
+                if (sc.nb > 0) b += t0[h] + t1[h] + t2[h];
+                o[h] = b;
+            }
+        }
+    }
+};
 
 // Sum over the slots of a wave, in slot 0.
 __device__ __forceinline__ float slots_sum(float v, int S, int step, int slot, int lane) {
@@ -189,19 +265,23 @@ __device__ __forceinline__ float slots_max(float v, int S, int step, int slot, i
     return v;
 }
 
-// Which lists the waves take. Units (a row, or S rows of a cloud with EACH)
-// are laid out so that an XCD's workgroups walk through one range of them side
-// by side: groups near each other share points, and share the XCD's L2.
+// Which lists the waves take. A unit is a row, or S * P rows of a cloud (P for
+// each slot). Units are laid out so that an XCD's workgroups walk through one
+// range of them side by side: groups near each other share points, and share
+// the XCD's L2.
 struct Walk {
-    int64_t units;     // per launch
-    int32_t per_cloud; // EACH: units per cloud
+    int64_t units;
+    int32_t per_cloud;  // units
+    int32_t P;
     Magic by_cloud;
 };
 
-template <bool EACH>
-Walk make_walk(int32_t B, int32_t rows_per_cloud, const Lanes& l) {
+// `slots`: slots that take rows of their own (1: a row to the wave).
+Walk make_walk(int32_t B, int32_t rows_per_cloud, int32_t slots, int32_t P) {
     Walk w;
-    w.per_cloud = EACH ? (rows_per_cloud + l.S - 1) / l.S : rows_per_cloud;
+    w.P = P;
+    const int64_t per = (int64_t)slots * P;
+    w.per_cloud = (int32_t)((rows_per_cloud + per - 1) / per);
     w.units = (int64_t)B * w.per_cloud;
     w.by_cloud = make_magic((uint32_t)w.per_cloud);
     return w;
@@ -215,6 +295,27 @@ __device__ __forceinline__ void each_unit(int64_t units, int per, int mine, F f)
     for (int64_t u = lo + i * per + mine; u < hi; u += n * per) f((uint32_t)__builtin_amdgcn_readfirstlane((int)u));
 }
 
+// Rows loaded at once: U of each slot. Entries of a chunk: with EACH as many as
+// a slot has lanes, else one per lane of the wave.
+template <bool EACH, int U>
+struct Rounds {
+    static __host__ __device__ int slot_rows(const Lanes& l) { return (l.Hc * l.G + U - 1) / U * U; }
+    static __host__ __device__ int rows_n(const Lanes& l) {
+        if (EACH) return l.S * slot_rows(l);
+        const int per = U * l.S;
+        return (kWave + per - 1) / per * per;
+    }
+    int chunk, first, by, per;  // entries; the slot's first row; from one of the U rows to the next; a round's entries
+
+    __device__ __forceinline__ Rounds(const Lanes& l, int slot) {
+        const int s = slot < l.S ? slot : 0;
+        chunk = EACH ? l.Hc * l.G : kWave;
+        first = EACH ? s * slot_rows(l) : s;
+        by = EACH ? 1 : l.S;
+        per = EACH ? U : U * l.S;
+    }
+};
+
 // Partial softmax of a part of a list: maximum and sum, and the weighted sum's
 // D channels, per row and head.
 struct Partial {
@@ -223,36 +324,44 @@ struct Partial {
     int32_t parts;
 };
 
+template <typename T>
+__device__ __forceinline__ uint32_t cloud_bytes(int32_t rows, int64_t row, int32_t last) {
+    return (uint32_t)(((rows - 1) * row + last) * (int64_t)sizeof(T));
+}
+
+template <int R>
+constexpr int kUnroll = R == 4 ? 2 : 4;
+
 // R: query heads a lane holds (they share the key's head).
 template <typename T, bool BUF, int R, bool EACH, bool BLOCK>
 __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lanes l, Walk walk, T* __restrict__ out,
                                                    float* __restrict__ lse, Partial part) {
     constexpr int W = kVec<T>;
-    constexpr int U = R == 4 ? 2 : 4;
-    extern __shared__ float s_lds[];
+    constexpr int U = kUnroll<R>;
+    extern __shared__ __align__(16) float s_lds[];
     const Score sc(b, a, s_lds);
-    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    const int lane = lane_id(), wave = threadIdx.x / kWave, waves_b = blockDim.x / kWave;
     const LaneAt at(l, a.H / R, a.D, W);
-    const int h0 = at.head * R;
+    const Rounds<EACH, U> rd(l, at.slot);
+    const int rows_n = Rounds<EACH, U>::rows_n(l), hp = l.Hc * R, hw = (int)blockIdx.y * hp;
+    const int hn = a.H - hw < hp ? a.H - hw : hp;  // heads of this pass
+    Chunk ck(s_lds + Score::floats(b), rows_n, sc, hp);
+    const int h0 = at.head * R, hl = at.on ? h0 - hw : 0;
     const int kvh = h0 / (a.H / a.Hkv);
     const int step = l.Hc * l.G;
     const uint32_t krb = (uint32_t)(a.k_row * (int64_t)sizeof(T)), vrb = (uint32_t)(a.v_row * (int64_t)sizeof(T));
-    const bool same = krb == vrb;
-    float slope[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) slope[r] = b.slope && at.on ? b.slope[h0 + r] : 0.0f;
+    const uint32_t kbytes = cloud_bytes<T>(g.N, a.k_row, a.Hkv * a.D);
+    const uint32_t vbytes = cloud_bytes<T>(g.N, a.v_row, a.Hkv * a.D);
 
-    each_unit(walk.units, BLOCK ? 1 : kAtWaves, BLOCK ? 0 : wave, [&](uint32_t unit) {
+    each_unit(walk.units, BLOCK ? 1 : waves_b, BLOCK ? 0 : wave, [&](uint32_t unit) {
         const uint32_t cloud = udiv(unit, walk.by_cloud);
         const uint32_t in = unit - cloud * (uint32_t)walk.per_cloud;
         const int32_t j = EACH ? (int32_t)in * l.S + at.slot : (int32_t)in;
         const bool live_row = !EACH || (j < g.M && at.slot < l.S);
         const int64_t row = (int64_t)cloud * g.M + (live_row ? j : 0);
         const int64_t p0 = (int64_t)cloud * g.N;
-        const Rows<T, BUF> kr((const T*)a.k + p0 * a.k_row, a.k_row, (uint32_t)((g.N - 1) * (int64_t)krb) +
-                              (uint32_t)(a.Hkv * a.D * (int)sizeof(T)), kvh * a.D + at.chan, at.n);
-        const Rows<T, BUF> vr((const T*)a.v + p0 * a.v_row, a.v_row, (uint32_t)((g.N - 1) * (int64_t)vrb) +
-                              (uint32_t)(a.Hkv * a.D * (int)sizeof(T)), kvh * a.D + at.chan, at.n);
+        const Rows<T, BUF> kr((const T*)a.k + p0 * a.k_row, a.k_row, kbytes, kvh * a.D + at.chan, at.n);
+        const Rows<T, BUF> vr((const T*)a.v + p0 * a.v_row, a.v_row, vbytes, kvh * a.D + at.chan, at.n);
         Raw q[R];
         float acc[R][W] = {}, m[R], sum[R];
 #pragma unroll
@@ -266,52 +375,44 @@ __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lan
         int64_t beg, end;
         g.range((int32_t)row, beg, end);
         if (EACH && !live_row) end = beg;
-        const int split = BLOCK ? kAtWaves * part.parts : part.parts;
-        if (!EACH && split > 1) {
+        if (!EACH && (BLOCK || part.parts > 1)) {
+            const int split = BLOCK ? waves_b * part.parts : part.parts;
             const int64_t per = (end - beg + split - 1) / split;
-            beg += (BLOCK ? (int64_t)blockIdx.z * kAtWaves + wave : (int64_t)blockIdx.z) * per;
+            beg += (BLOCK ? (int64_t)blockIdx.z * waves_b + wave : (int64_t)blockIdx.z) * per;
             end = end < beg + per ? end : beg + per;
         }
-        const int ch = EACH ? step : kWave;  // entries of a chunk
-        const int first = EACH ? at.slot * step : at.slot;
-        for (int64_t s0 = beg; EACH ? __any(s0 < end) : s0 < end; s0 += ch) {
-            const int n = end - s0 < ch ? (int)(end - s0) : ch;
-            int32_t mine = -1;
+        for (int64_t s0 = beg; EACH ? __any(s0 < end) : s0 < end; s0 += rd.chunk) {
+            const int n = end - s0 < rd.chunk ? (int)(end - s0) : rd.chunk;
+            const int e = EACH ? at.li : lane;
+            int32_t mine = kNoEntry;
             uint32_t u = 0;
             float dist = 0.0f;
-            const int e = EACH ? at.li : lane;
             if (e < n) {
                 mine = g.idx[s0 + e];
-                if ((uint32_t)mine >= (uint32_t)g.N) mine = -1;
+                if ((uint32_t)mine >= (uint32_t)g.N) mine = kMasked;
                 if (sc.placed() && mine >= 0) {
                     float p[3];
                     load_xyz(g.points, p0 + mine, p);
                     pair_place(sc.ed, sc.dist, p, c, u, dist);
                 }
             }
-            const uint32_t kkey = Rows<T, BUF>::key(mine, krb), vkey = Rows<T, BUF>::key(mine, vrb);
-            for (int t = 0; EACH ? __any(t < n) : t < n; t += EACH ? U : U * l.S) {
+            if (!EACH || at.slot < l.S)
+                ck.put(EACH ? rd.first + e : e, Rows<T, BUF>::key(mine, krb), Rows<T, BUF>::key(mine, vrb), mine, u,
+                       dist, sc, hw, hn);
+            __builtin_amdgcn_wave_barrier();
+            for (int t = 0; EACH ? __any(t < n) : t < n; t += rd.per) {
                 Raw k[U], v[U];
-                uint32_t pu[U];
-                float pd[U], s[U * R];
+                float s[U * R], bi[U * R];
                 bool there[U];
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
-                    const int from = EACH ? t + i : t + i * l.S + at.slot;
-                    const int src = (EACH ? first + from : from) & 63;
-                    uint32_t key = (uint32_t)__shfl((int)kkey, src, kWave);
-                    if (from >= n) key = 0xFFFFFFFFu & (BUF ? kNone : 0xFFFFFFFFu);
+                    const float* r0 = ck.row(rd.first + t + i * rd.by);
+                    const uint32_t key = ck.field(r0, kKey);
                     there[i] = Rows<T, BUF>::there(key);
                     k[i] = kr.load(key);
-                    if (!BUF || same) {
-                        v[i] = vr.load(key);
-                    } else {
-                        const uint32_t key2 = (uint32_t)__shfl((int)vkey, src, kWave);
-                        v[i] = vr.load(there[i] ? key2 : kNone);
-                    }
-                    if (sc.nb > 0) pu[i] = (uint32_t)__shfl((int)u, src, kWave);
-                    else pu[i] = 0;
-                    pd[i] = sc.dist ? __shfl(dist, src, kWave) : 0.0f;
+                    v[i] = vr.load(ck.field(r0, kKey2));
+#pragma unroll
+                    for (int r = 0; r < R; ++r) bi[i * R + r] = sc.placed() ? r0[hl + r] : 0.0f;
                 }
 #pragma unroll
                 for (int i = 0; i < U; ++i)
@@ -323,15 +424,13 @@ __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lan
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
                         float e2;
-                        float x = sc.product(s[i * R + r], e2);
-                        if (sc.placed()) {
-                            const float bi = sc.bias(h0 + r, pu[i], slope[r], pd[i]);
-                            x = bi == kNegInf ? kNegInf : x + bi;
-                            if (R == 1 && __any(bi == kNegInf)) {  // masked by the bias: whatever v holds
-                                if (bi == kNegInf) v[i] = Raw{0, 0, 0, 0};
-                            }
+                        const float x = sc.product(s[i * R + r], e2) + bi[i * R + r];
+                        // masked by the bias: whatever k and v hold
+                        const bool off = bi[i * R + r] == kNegInf || !there[i];
+                        if (R == 1 && __any(off && there[i])) {
+                            if (off) v[i] = Raw{0, 0, 0, 0};
                         }
-                        s[i * R + r] = there[i] ? x : kNegInf;
+                        s[i * R + r] = off ? kNegInf : x;
                     }
                 }
 #pragma unroll
@@ -361,6 +460,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lan
                     }
                 }
             }
+            __builtin_amdgcn_wave_barrier();
         }
         if (!EACH) {  // the slots' parts joined in slot 0
 #pragma unroll
@@ -376,12 +476,12 @@ __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lan
         const bool writes = EACH ? at.on && live_row : at.on && at.slot == 0;
         if constexpr (BLOCK) {
             // the waves' parts joined in LDS: [wave][heads of this pass][D + 2]
-            const int D2 = a.D + 2, hp = l.Hc * R;
-            float* s_join = s_lds + Score::floats(b);
+            const int D2 = a.D + 2;
+            float* s_join = s_lds + Score::floats(b) + waves_b * Chunk::floats(sc.placed(), rows_n, hp);
             if (writes) {
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    float* d = s_join + (wave * hp + h0 - (int)blockIdx.y * hp + r) * D2;
+                    float* d = s_join + (wave * hp + hl + r) * D2;
                     if (at.chan == 0) {
                         d[0] = m[r];
                         d[1] = sum[r];
@@ -392,22 +492,19 @@ __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lan
                 }
             }
             __syncthreads();
-            const int hq = a.H - (int)blockIdx.y * hp < hp ? a.H - (int)blockIdx.y * hp : hp;
-            for (int e = threadIdx.x; e < hq * a.D; e += kAtThreads) {
+            for (int e = threadIdx.x; e < hn * a.D; e += blockDim.x) {
                 const int h = e / a.D, d = e - h * a.D;
                 const float* s = s_join + h * D2;
                 float mm = kNegInf;
-#pragma unroll
-                for (int w = 0; w < kAtWaves; ++w) mm = fmaxf(mm, s[w * hp * D2]);
+                for (int w = 0; w < waves_b; ++w) mm = fmaxf(mm, s[w * hp * D2]);
                 const float z = mm == kNegInf ? 0.0f : mm;
                 float x = 0.0f, total = 0.0f;
-#pragma unroll
-                for (int w = 0; w < kAtWaves; ++w) {
+                for (int w = 0; w < waves_b; ++w) {
                     const float f = weight(s[w * hp * D2] - z);
                     total = fmaf(s[w * hp * D2 + 1], f, total);
                     x = fmaf(s[w * hp * D2 + 2 + d], f, x);
                 }
-                const int64_t rh = row * a.H + (int)blockIdx.y * hp + h;
+                const int64_t rh = row * a.H + hw + h;
                 if (part.parts > 1) {
                     const int64_t prh = (int64_t)blockIdx.z * g.rows * a.H + rh;
                     if (d == 0) {
@@ -417,8 +514,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lan
                     part.acc[prh * a.D + d] = x;
                 } else {
                     out[rh * a.D + d] = (T)(total == 0.0f ? 0.0f : x / total);
-                    if (lse && d == 0)
-                        lse[rh] = total == 0.0f ? kNegInf : mm + log_sum(total);
+                    if (lse && d == 0) lse[rh] = total == 0.0f ? kNegInf : mm + log_sum(total);
                 }
             }
             __syncthreads();
@@ -478,28 +574,29 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
                                                           const float* __restrict__ lse, const T* __restrict__ dout,
                                                           T* __restrict__ dq, float2* __restrict__ stat) {
     constexpr int W = kVec<T>;
-    constexpr int U = 4;
-    extern __shared__ float s_lds[];
+    constexpr int U = kUnroll<1>;
+    extern __shared__ __align__(16) float s_lds[];
     const Score sc(b, a, s_lds);
-    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    const int lane = lane_id(), wave = threadIdx.x / kWave, waves_b = blockDim.x / kWave;
     const LaneAt at(l, a.H, a.D, W);
+    const Rounds<EACH, U> rd(l, at.slot);
+    const int hw = (int)blockIdx.y * l.Hc, hn = a.H - hw < l.Hc ? a.H - hw : l.Hc, hl = at.on ? at.head - hw : 0;
+    Chunk ck(s_lds + Score::floats(b), Rounds<EACH, U>::rows_n(l), sc, l.Hc);
     const int kvh = at.head / (a.H / a.Hkv);
     const int step = l.Hc * l.G;
     const uint32_t krb = (uint32_t)(a.k_row * (int64_t)sizeof(T)), vrb = (uint32_t)(a.v_row * (int64_t)sizeof(T));
-    const bool same = krb == vrb;
-    const float slope = b.slope && at.on ? b.slope[at.head] : 0.0f;
+    const uint32_t kbytes = cloud_bytes<T>(g.N, a.k_row, a.Hkv * a.D);
+    const uint32_t vbytes = cloud_bytes<T>(g.N, a.v_row, a.Hkv * a.D);
 
-    each_unit(walk.units, kAtWaves, wave, [&](uint32_t unit) {
+    each_unit(walk.units, waves_b, wave, [&](uint32_t unit) {
         const uint32_t cloud = udiv(unit, walk.by_cloud);
         const uint32_t in = unit - cloud * (uint32_t)walk.per_cloud;
         const int32_t j = EACH ? (int32_t)in * l.S + at.slot : (int32_t)in;
         const bool live_row = !EACH || (j < g.M && at.slot < l.S);
         const int64_t row = (int64_t)cloud * g.M + (live_row ? j : 0);
         const int64_t p0 = (int64_t)cloud * g.N;
-        const Rows<T, BUF> kr((const T*)a.k + p0 * a.k_row, a.k_row, (uint32_t)((g.N - 1) * (int64_t)krb) +
-                              (uint32_t)(a.Hkv * a.D * (int)sizeof(T)), kvh * a.D + at.chan, at.n);
-        const Rows<T, BUF> vr((const T*)a.v + p0 * a.v_row, a.v_row, (uint32_t)((g.N - 1) * (int64_t)vrb) +
-                              (uint32_t)(a.Hkv * a.D * (int)sizeof(T)), kvh * a.D + at.chan, at.n);
+        const Rows<T, BUF> kr((const T*)a.k + p0 * a.k_row, a.k_row, kbytes, kvh * a.D + at.chan, at.n);
+        const Rows<T, BUF> vr((const T*)a.v + p0 * a.v_row, a.v_row, vbytes, kvh * a.D + at.chan, at.n);
         const int64_t rh = row * a.H + at.head;
         const Raw q = load_channels<T, BUF>((const T*)a.q + row * a.q_row + at.head * a.D + at.chan, at.n);
         const Raw go = load_channels<T, BUF>(dout + rh * a.D + at.chan, at.n);
@@ -511,46 +608,37 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
         int64_t beg, end;
         g.range((int32_t)row, beg, end);
         if (EACH && !live_row) end = beg;
-        const int ch = EACH ? step : kWave;
-        const int first = EACH ? at.slot * step : at.slot;
-        for (int64_t s0 = beg; EACH ? __any(s0 < end) : s0 < end; s0 += ch) {
-            const int n = end - s0 < ch ? (int)(end - s0) : ch;
-            int32_t mine = -1;
+        for (int64_t s0 = beg; EACH ? __any(s0 < end) : s0 < end; s0 += rd.chunk) {
+            const int n = end - s0 < rd.chunk ? (int)(end - s0) : rd.chunk;
+            const int e = EACH ? at.li : lane;
+            int32_t mine = kNoEntry;
             uint32_t u = 0;
             float dist = 0.0f;
-            const int e = EACH ? at.li : lane;
             if (e < n) {
                 mine = g.idx[s0 + e];
-                if ((uint32_t)mine >= (uint32_t)g.N) mine = -1;
+                if ((uint32_t)mine >= (uint32_t)g.N) mine = kMasked;
                 if (sc.placed() && mine >= 0) {
                     float p[3];
                     load_xyz(g.points, p0 + mine, p);
                     pair_place(sc.ed, sc.dist, p, c, u, dist);
                 }
             }
-            const uint32_t kkey = Rows<T, BUF>::key(mine, krb), vkey = Rows<T, BUF>::key(mine, vrb);
-            for (int t = 0; EACH ? __any(t < n) : t < n; t += EACH ? U : U * l.S) {
+            if (!EACH || at.slot < l.S)
+                ck.put(EACH ? rd.first + e : e, Rows<T, BUF>::key(mine, krb), Rows<T, BUF>::key(mine, vrb), mine, u,
+                       dist, sc, hw, hn);
+            __builtin_amdgcn_wave_barrier();
+            for (int t = 0; EACH ? __any(t < n) : t < n; t += rd.per) {
                 Raw k[U], v[U];
-                uint32_t pu[U];
-                float pd[U], s[2 * U];
+                float s[2 * U], bi[U];
                 bool there[U];
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
-                    const int from = EACH ? t + i : t + i * l.S + at.slot;
-                    const int src = (EACH ? first + from : from) & 63;
-                    uint32_t key = (uint32_t)__shfl((int)kkey, src, kWave);
-                    if (from >= n) key = BUF ? kNone : 0xFFFFFFFFu;
+                    const float* r0 = ck.row(rd.first + t + i * rd.by);
+                    const uint32_t key = ck.field(r0, kKey);
                     there[i] = Rows<T, BUF>::there(key);
                     k[i] = kr.load(key);
-                    if (!BUF || same) {
-                        v[i] = vr.load(key);
-                    } else {
-                        const uint32_t key2 = (uint32_t)__shfl((int)vkey, src, kWave);
-                        v[i] = vr.load(there[i] ? key2 : kNone);
-                    }
-                    if (sc.nb > 0) pu[i] = (uint32_t)__shfl((int)u, src, kWave);
-                    else pu[i] = 0;
-                    pd[i] = sc.dist ? __shfl(dist, src, kWave) : 0.0f;
+                    v[i] = vr.load(ck.field(r0, kKey2));
+                    bi[i] = sc.placed() ? r0[hl] : 0.0f;
                 }
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
@@ -561,16 +649,12 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
                     float e2 = 0.0f, dp = s[2 * i + 1];
-                    float x = sc.product(s[2 * i], e2);
-                    if (sc.placed()) {
-                        const float bi = sc.bias(at.head, pu[i], slope, pd[i]);
-                        x += bi;
-                        if (__any(bi == kNegInf)) {  // masked by the bias: whatever k and v hold
-                            if (bi == kNegInf) {
-                                k[i] = Raw{0, 0, 0, 0};
-                                x = kNegInf;
-                                dp = 0.0f;
-                            }
+                    float x = sc.product(s[2 * i], e2) + bi[i];
+                    if (__any(bi[i] == kNegInf)) {  // masked by the bias: whatever k and v hold
+                        if (bi[i] == kNegInf) {
+                            k[i] = Raw{0, 0, 0, 0};
+                            x = kNegInf;
+                            dp = 0.0f;
                         }
                     }
                     const float p = there[i] ? weight(x - z) : 0.0f;
@@ -581,6 +665,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
                     add_channels<T>(acd, p * sl, k[i]);
                 }
             }
+            __builtin_amdgcn_wave_barrier();
         }
         if (!EACH) {
             sum = slots_sum(sum, l.S, step, at.slot, lane);
@@ -602,7 +687,14 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
 
 // Gradient at the points, over the centers that hold each; and the bias's
 // gradient, which a wave sums in a table of its own in LDS.
-template <typename T, bool BUF, bool EACH, bool TAB>
+// FLAT: a slot takes P points in a row and walks through their lists as one
+// (lists here are a few entries long: a list per slot would leave most of a
+// round's rows empty, and the wave would wait for the longest). A round's rows
+// are then of any of its points, so that each entry brings its point's k and v
+// rows along, which the L1 holds; the sums are written when the point changes.
+constexpr int kBackUnroll = 2;
+
+template <typename T, bool BUF, bool FLAT, bool TAB>
 __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn a, Lanes l, Walk walk,
                                                           const int64_t* __restrict__ pt_off,
                                                           const int32_t* __restrict__ pt_center, int64_t capacity,
@@ -610,135 +702,214 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                                                           T* __restrict__ dk, T* __restrict__ dv,
                                                           float* __restrict__ part) {
     constexpr int W = kVec<T>;
-    constexpr int U = 4;
-    extern __shared__ float s_lds[];
+    constexpr int U = kBackUnroll;
+    extern __shared__ __align__(16) float s_lds[];
     const Score sc(b, a, s_lds);
     const int lane = lane_id(), wave = threadIdx.x / kWave, waves_b = blockDim.x / kWave;
+    const int Rq = a.H / a.Hkv;
+    const LaneAt at(l, a.Hkv, a.D, W);
+    const Rounds<FLAT, U> rd(l, at.slot);
+    const int rows_n = Rounds<FLAT, U>::rows_n(l), hp = l.Hc * Rq, hw = (int)blockIdx.y * hp;
+    const int hn = a.H - hw < hp ? a.H - hw : hp;
+    Chunk ck(s_lds + Score::floats(b), rows_n, sc, hp);
     const int entries = (3 * b.nb + 1) * a.H;
-    float* s_tab = s_lds + Score::floats(b);
+    float* s_tab = s_lds + Score::floats(b) + waves_b * Chunk::floats(sc.placed(), rows_n, hp);
     float* tab = s_tab + wave * entries;
     if constexpr (TAB) {
         for (int e = threadIdx.x; e < entries * waves_b; e += blockDim.x) s_tab[e] = 0.0f;
         __syncthreads();
     }
-    const LaneAt at(l, a.Hkv, a.D, W);
-    const int Rq = a.H / a.Hkv;
-    const int step = l.Hc * l.G;
+    const int step = l.Hc * l.G, slot = at.slot < l.S ? at.slot : 0;
     const uint32_t qrb = (uint32_t)(a.q_row * (int64_t)sizeof(T)), orb = (uint32_t)(a.H * a.D * (int)sizeof(T));
-    const bool same = qrb == orb;
+    const uint32_t qbytes = cloud_bytes<T>(g.M, a.q_row, a.H * a.D);
+    const uint32_t gbytes = cloud_bytes<T>(g.M, (int64_t)a.H * a.D, a.H * a.D);
 
     each_unit(walk.units, waves_b, wave, [&](uint32_t unit) {
         const uint32_t cloud = udiv(unit, walk.by_cloud);
         const uint32_t in = unit - cloud * (uint32_t)walk.per_cloud;
-        const int32_t i0 = EACH ? (int32_t)in * l.S + at.slot : (int32_t)in;
-        const bool live_row = !EACH || (i0 < g.N && at.slot < l.S);
-        const int64_t pt = (int64_t)cloud * g.N + (live_row ? i0 : 0);
-        const int64_t c0 = (int64_t)cloud * g.M;
-        const Raw x = load_channels<T, BUF>((const T*)a.k + pt * a.k_row + at.head * a.D + at.chan, at.n);
-        const Raw y = load_channels<T, BUF>((const T*)a.v + pt * a.v_row + at.head * a.D + at.chan, at.n);
-        float gk[W] = {}, gv[W] = {}, p3[3] = {};
-        if (sc.placed()) load_xyz(g.points, pt, p3);
-        int64_t beg = pt_off[pt], end = pt_off[pt + 1];
-        beg = beg < 0 ? 0 : beg > capacity ? capacity : beg;
-        end = end < beg ? beg : end > capacity ? capacity : end;
-        if (EACH && !live_row) end = beg;
-        const int ch = EACH ? step : kWave;
-        const int first = EACH ? at.slot * step : at.slot;
-        for (int64_t s0 = beg; EACH ? __any(s0 < end) : s0 < end; s0 += ch) {
-            const int n = end - s0 < ch ? (int)(end - s0) : ch;
-            int32_t mine = -1;
+        const int64_t p0 = (int64_t)cloud * g.N, c0 = (int64_t)cloud * g.M;
+        // the slot's points: n0 of them from i0 on
+        int32_t i0 = (int32_t)in, n0 = 1;
+        if (FLAT) {
+            const int64_t f = ((int64_t)in * l.S + at.slot) * walk.P;
+            n0 = at.slot < l.S && f < g.N ? (g.N - f < walk.P ? (int32_t)(g.N - f) : walk.P) : 0;
+            i0 = n0 ? (int32_t)f : 0;
+        }
+        const Rows<T, BUF> qr((const T*)a.q + c0 * a.q_row, a.q_row, qbytes, at.head * Rq * a.D + at.chan, at.n);
+        const Rows<T, BUF> gr(dout + c0 * a.H * a.D, (int64_t)a.H * a.D, gbytes, at.head * Rq * a.D + at.chan, at.n);
+        auto clip = [&](int64_t x) { return x < 0 ? 0 : x > capacity ? capacity : x; };
+        const int64_t beg = clip(pt_off[p0 + i0]);
+        int64_t total = clip(pt_off[p0 + i0 + n0]) - beg;
+        if (total < 0) total = 0;
+        const int64_t o = ((p0 + i0) * a.Hkv + at.head) * a.D + at.chan;  // of the first point's sums
+        const int64_t by = (int64_t)a.Hkv * a.D;
+        float gk[W] = {}, gv[W] = {};
+        Raw x, y;
+        float p3[3] = {};
+        int32_t starts = 0, cur = -1;  // FLAT: where the lane's point's list starts; the point the sums are of
+        if (FLAT) {
+            // points without an entry get zeros
+            int64_t f = at.li < n0 ? clip(pt_off[p0 + i0 + at.li]) - beg : total;
+            f = f < 0 ? 0 : f > total ? total : f;
+            starts = (int32_t)f;
+            int32_t next = __shfl(starts, (lane + 1) & 63, kWave);
+            if (at.li + 1 >= n0 || at.li + 1 >= step) next = (int32_t)total;
+            uint64_t none = __ballot(at.slot < l.S && at.li < n0 && starts >= next) >> (slot * step);
+            none &= (1ull << n0) - 1;  // n0 <= kPoints
+            while (__any(none != 0)) {
+                if (none && at.on) {
+                    const int32_t k = __ffsll((unsigned long long)none) - 1;
+                    store_channels<T, BUF>(dk + o + k * by, at.n, gk);
+                    store_channels<T, BUF>(dv + o + k * by, at.n, gv);
+                }
+                none &= none - 1;
+            }
+        } else {
+            x = load_channels<T, BUF>((const T*)a.k + (p0 + i0) * a.k_row + at.head * a.D + at.chan, at.n);
+            y = load_channels<T, BUF>((const T*)a.v + (p0 + i0) * a.v_row + at.head * a.D + at.chan, at.n);
+            if (sc.placed()) load_xyz(g.points, p0 + i0, p3);
+        }
+        auto write = [&](int32_t k) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) gk[w] *= a.scale;
+            store_channels<T, BUF>(dk + o + k * by, at.n, gk);
+            store_channels<T, BUF>(dv + o + k * by, at.n, gv);
+        };
+        for (int64_t s0 = 0; FLAT ? __any(s0 < total) : s0 < total; s0 += rd.chunk) {
+            const int n = total - s0 < rd.chunk ? (int)(total - s0) : rd.chunk;
+            const int e = FLAT ? at.li : lane;
+            int32_t mine = kNoEntry, k = 0;
             uint32_t u = 0;
             float dist = 0.0f;
-            const int e = EACH ? at.li : lane;
+            if (FLAT) {  // the last point whose list starts at or before the entry
+#pragma unroll
+                for (int h = kPoints / 2; h > 0; h >>= 1) {
+                    const int32_t st = __shfl(starts, slot * step + (k + h < step ? k + h : 0), kWave);
+                    if (k + h < n0 && st <= (int32_t)s0 + e) k += h;
+                }
+            }
             if (e < n) {
-                mine = pt_center[s0 + e];
-                if ((uint32_t)mine >= (uint32_t)g.M) mine = -1;
+                mine = pt_center[beg + s0 + e];
+                if ((uint32_t)mine >= (uint32_t)g.M) mine = kMasked;
                 if (sc.placed() && mine >= 0) {
                     float c[3];
                     load_xyz(g.centers, c0 + mine, c);
+                    if (FLAT) load_xyz(g.points, p0 + i0 + k, p3);
                     pair_place(sc.ed, sc.dist, p3, c, u, dist);
                 }
             }
-            for (int r = 0; r < Rq; ++r) {
-                const int h = at.head * Rq + r;
-                const Rows<T, BUF> qr((const T*)a.q + c0 * a.q_row, a.q_row, (uint32_t)((g.M - 1) * (int64_t)qrb) + orb,
-                                      h * a.D + at.chan, at.n);
-                const Rows<T, BUF> gr(dout + c0 * a.H * a.D, (int64_t)a.H * a.D, (uint32_t)(g.M * (int64_t)orb),
-                                      h * a.D + at.chan, at.n);
-                const float slope = b.slope && at.on ? b.slope[h] : 0.0f;
-                for (int t = 0; EACH ? __any(t < n) : t < n; t += EACH ? U : U * l.S) {
-                    Raw q[U], go[U];
-                    uint32_t pu[U];
-                    float pd[U], s[2 * U];
-                    float2 st[U];
-                    bool there[U];
+            if (!FLAT || at.slot < l.S) {
+                const int r = FLAT ? rd.first + e : e;
+                ck.put(r, Rows<T, BUF>::key(mine, qrb), Rows<T, BUF>::key(mine, orb), mine, u, dist, sc, hw, hn);
+                if (FLAT) ck.rows[r * ck.stride + ck.hp + kPoint] = __int_as_float(k);
+            }
+            __builtin_amdgcn_wave_barrier();
+            // Entries one after another, the heads that share a key within each (FLAT: an entry's point must not
+            // come back once the sums are another's).
+            const int all = FLAT ? n * Rq : (n + rd.per - 1) / rd.per * Rq;
+            for (int t = 0; FLAT ? __any(t < all) : t < all; t += FLAT ? U : 1) {
+                int at_row[U], rr[U];
 #pragma unroll
-                    for (int i = 0; i < U; ++i) {
-                        const int from = EACH ? t + i : t + i * l.S + at.slot;
-                        const int src = (EACH ? first + from : from) & 63;
-                        int32_t jj = __shfl(mine, src, kWave);
-                        if (from >= n) jj = -1;
-                        there[i] = jj >= 0;
-                        const uint32_t key = Rows<T, BUF>::key(jj, qrb);
-                        q[i] = qr.load(key);
-                        go[i] = gr.load(!BUF || same ? key : Rows<T, BUF>::key(jj, orb));
-                        st[i] = stat[(c0 + (there[i] ? jj : 0)) * a.H + h];
-                        if (sc.nb > 0) pu[i] = (uint32_t)__shfl((int)u, src, kWave);
-                        else pu[i] = 0;
-                        pd[i] = sc.dist ? __shfl(dist, src, kWave) : 0.0f;
+                for (int i = 0; i < U; ++i) {
+                    const int m = FLAT ? t + i : t, en = Rq == 1 ? m : m / Rq;
+                    rr[i] = m - en * Rq;
+                    at_row[i] = rd.first + (FLAT ? en : en * rd.per + i * rd.by);
+                }
+                Raw q[U], go[U], kx[U], vx[U];
+                float s[2 * U], bi[U], pd[U];
+                float2 st[U];
+                uint32_t pu[U];
+                int32_t pk[U];
+                bool there[U];
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    const int h = at.head * Rq + rr[i];
+                    const uint32_t head_off = BUF ? (uint32_t)(rr[i] * a.D * (int)sizeof(T)) : 0u;
+                    const float* r0 = ck.row(at_row[i]);
+                    const int32_t jj = (int32_t)ck.field(r0, kIndex);
+                    there[i] = jj >= 0;
+                    const uint32_t key = ck.field(r0, kKey), key2 = ck.field(r0, kKey2);
+                    if constexpr (BUF) {
+                        q[i] = qr.load(key + head_off);
+                        go[i] = gr.load(key2 + head_off);
+                    } else {
+                        const int64_t row = c0 + (there[i] ? jj : 0);
+                        q[i] = load_channels<T, false>((const T*)a.q + row * a.q_row + h * a.D + at.chan, at.n);
+                        go[i] = load_channels<T, false>(dout + (row * a.H + h) * a.D + at.chan, at.n);
                     }
-#pragma unroll
-                    for (int i = 0; i < U; ++i) {
-                        s[2 * i] = dot<T>(q[i], x);
-                        s[2 * i + 1] = dot<T>(go[i], y);
+                    st[i] = stat[(c0 + (there[i] ? jj : 0)) * a.H + h];
+                    pk[i] = 0;
+                    if (FLAT) {
+                        pk[i] = jj != kNoEntry ? (int32_t)ck.field(r0, kPoint) : -1;
+                        const int64_t pt = p0 + i0 + (pk[i] > 0 ? pk[i] : 0);
+                        kx[i] = load_channels<T, BUF>((const T*)a.k + pt * a.k_row + at.head * a.D + at.chan, at.n);
+                        vx[i] = load_channels<T, BUF>((const T*)a.v + pt * a.v_row + at.head * a.D + at.chan, at.n);
+                    } else {
+                        kx[i] = x;
+                        vx[i] = y;
                     }
-                    group_sums(s, l.G);
+                    bi[i] = sc.placed() ? r0[at.on ? h - hw : 0] : 0.0f;
+                    pu[i] = ck.field(r0, kPlace);
+                    pd[i] = r0[ck.hp + kDist];
+                }
 #pragma unroll
-                    for (int i = 0; i < U; ++i) {
-                        float e2 = 0.0f, dp = s[2 * i + 1];
-                        float v = sc.product(s[2 * i], e2);
-                        if (sc.placed()) {
-                            const float bi = sc.bias(h, pu[i], slope, pd[i]);
-                            v += bi;
-                            if (__any(bi == kNegInf)) {
-                                if (bi == kNegInf) {
-                                    q[i] = go[i] = Raw{0, 0, 0, 0};
-                                    v = kNegInf;
-                                    dp = 0.0f;
-                                }
+                for (int i = 0; i < U; ++i) {
+                    s[2 * i] = dot<T>(q[i], kx[i]);
+                    s[2 * i + 1] = dot<T>(go[i], vx[i]);
+                }
+                group_sums(s, l.G);
+#pragma unroll
+                for (int i = 0; i < U; ++i) {
+                    const int h = at.head * Rq + rr[i];
+                    float e2 = 0.0f, dp = s[2 * i + 1];
+                    float v = sc.product(s[2 * i], e2) + bi[i];
+                    if (__any(bi[i] == kNegInf)) {
+                        if (bi[i] == kNegInf) {
+                            q[i] = go[i] = Raw{0, 0, 0, 0};
+                            v = kNegInf;
+                            dp = 0.0f;
+                        }
+                    }
+                    const float p = there[i] ? weight(v - st[i].x) : 0.0f;
+                    const float ds = there[i] ? p * (dp - st[i].y) : 0.0f;
+                    const float da = there[i] ? ds * sc.slack(e2) : 0.0f;
+                    if (FLAT) {
+                        const bool change = pk[i] >= 0 && pk[i] != cur;
+                        if (__any(change)) {
+                            if (change) {
+                                if (cur >= 0) write(cur);
+#pragma unroll
+                                for (int w = 0; w < W; ++w) gk[w] = gv[w] = 0.0f;
+                                cur = pk[i];
                             }
                         }
-                        const float p = there[i] ? weight(v - st[i].x) : 0.0f;
-                        const float ds = there[i] ? p * (dp - st[i].y) : 0.0f;
-                        add_channels<T>(gk, ds * sc.slack(e2), q[i]);
-                        add_channels<T>(gv, p, go[i]);
-                        if constexpr (TAB) {
-                            if (at.chan == 0 && there[i] && at.on) {
-                                if (b.nb > 0) {
-                                    lds_add(&tab[(pu[i] & 255u) * a.H + h], ds);
-                                    lds_add(&tab[(b.nb + (pu[i] >> 8 & 255u)) * a.H + h], ds);
-                                    lds_add(&tab[(2 * b.nb + (pu[i] >> 16)) * a.H + h], ds);
-                                }
-                                if (b.slope) lds_add(&tab[3 * b.nb * a.H + h], ds * pd[i]);
+                    }
+                    add_channels<T>(gk, da, q[i]);
+                    add_channels<T>(gv, p, go[i]);
+                    if constexpr (TAB) {
+                        if (at.chan == 0 && there[i] && at.on) {
+                            if (b.nb > 0) {
+                                lds_add(&tab[(pu[i] & 255u) * a.H + h], ds);
+                                lds_add(&tab[(b.nb + (pu[i] >> 8 & 255u)) * a.H + h], ds);
+                                lds_add(&tab[(2 * b.nb + (pu[i] >> 16)) * a.H + h], ds);
                             }
+                            if (b.slope) lds_add(&tab[3 * b.nb * a.H + h], ds * pd[i]);
                         }
                     }
                 }
             }
+            __builtin_amdgcn_wave_barrier();
         }
-        if (!EACH) {
+        if (!FLAT) {
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 gk[w] = slots_sum(gk[w], l.S, step, at.slot, lane);
                 gv[w] = slots_sum(gv[w], l.S, step, at.slot, lane);
             }
+            if (at.on && at.slot == 0) write(0);
+        } else if (at.on && cur >= 0) {
+            write(cur);
         }
-        if (!(EACH ? at.on && live_row : at.on && at.slot == 0)) return;
-#pragma unroll
-        for (int w = 0; w < W; ++w) gk[w] *= a.scale;
-        const int64_t o = (pt * a.Hkv + at.head) * a.D + at.chan;
-        store_channels<T, BUF>(dk + o, at.n, gk);
-        store_channels<T, BUF>(dv + o, at.n, gv);
     });
     if constexpr (TAB) {
         __syncthreads();
@@ -762,6 +933,24 @@ bool each_of(int64_t rows, int64_t slots, const Lanes& l) {
     return slots / rows <= 32 && rows / l.S >= 4096;
 }
 
+// The launch of a kernel: waves of a workgroup, such that what they keep in
+// LDS fits, and LDS bytes.
+struct Shape {
+    int waves;
+    size_t lds;
+};
+
+Shape shape_of(const Bias& b, size_t floats_per_wave) {
+    const size_t base = (size_t)Score::floats(b) * 4;
+    Shape r;
+    r.waves = kAtWaves;
+    while (r.waves > 1 && base + floats_per_wave * 4 * r.waves > kAtLds) r.waves >>= 1;
+    r.lds = base + floats_per_wave * 4 * r.waves;
+    return r;
+}
+
+bool placed(const Bias& b) { return b.nb > 0 || b.slope; }
+
 // A workgroup to a list whose mean length gives each wave a chunk; parts where
 // there are few lists.
 struct Split {
@@ -769,13 +958,12 @@ struct Split {
     int32_t parts;
 };
 
-Split split_of(const Groups& g, int32_t passes, int32_t HD) {
+Split split_of(const Groups& g, int32_t HD) {
     Split s = {false, 1};
     const int64_t mean = g.idx_len / g.rows;  // of ragged lists only their mean is known here
-    const int64_t rows = (int64_t)g.rows * passes;
     if (mean < 2 * kWave || HD > kJoinFloats) return s;
     s.block = true;
-    int64_t p = 1024 / rows;
+    int64_t p = 1024 / g.rows;
     if (p > mean / (2 * kWave)) p = mean / (2 * kWave);
     s.parts = (int32_t)(p < 1 ? 1 : p > kWave ? kWave : p);
     return s;
@@ -793,9 +981,14 @@ bool vectors(const Groups& g, const Attn& a, std::initializer_list<const void*> 
     return a.k_row <= most / g.N && a.v_row <= most / g.N && a.q_row <= most / g.M && qd <= most / g.M;
 }
 
+// Query heads per lane: those that share a key's head, while the pass's heads
+// stay few (their biases of a chunk are in LDS).
+template <typename T>
 int heads_per_lane(const Attn& a) {
     const int r = a.H / a.Hkv;
-    return r % 4 == 0 ? 4 : r % 2 == 0 ? 2 : 1;
+    for (int R : {4, 2})
+        if (r % R == 0 && make_lanes<T>(a.H / R, a.D).Hc * R <= 64) return R;
+    return 1;
 }
 
 uint32_t blocks_of(int64_t units, int64_t per) {
@@ -809,36 +1002,18 @@ hipError_t allow_lds(K kern, size_t bytes) {
     return hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
 }
 
-template <typename T, bool BUF, int R>
-hipError_t forward_as(const Groups& g, int32_t B, const Attn& a, const Bias& b, void* out, float* lse, void* ws,
-                      hipStream_t s) {
-    const Lanes l = make_lanes<T>(a.H / R, a.D);
-    const Split sp = split_of(g, 1, a.H * a.D);
-    Partial part = {nullptr, nullptr, sp.parts};
-    if (part.parts > 1) {
-        part.ml = (float*)ws;
-        part.acc = part.ml + (size_t)part.parts * g.rows * a.H * 2;
-    }
-    size_t lds = (size_t)Score::floats(b) * 4;
-    hipError_t e = hipSuccess;
-    if (sp.block) {
-        const Walk w = make_walk<false>(B, g.M, l);
-        lds += (size_t)kAtWaves * l.Hc * R * (a.D + 2) * 4;
-        auto kern = k_at<T, BUF, R, false, true>;
-        if ((e = allow_lds(kern, lds)) != hipSuccess) return e;
-        kern<<<dim3(blocks_of(w.units, 1), l.passes, sp.parts), kAtThreads, lds, s>>>(g, b, a, l, w, (T*)out, lse,
-                                                                                     part);
-    } else if (each_of(g.rows, g.idx_len, l)) {
-        const Walk w = make_walk<true>(B, g.M, l);
-        auto kern = k_at<T, BUF, R, true, false>;
-        if ((e = allow_lds(kern, lds)) != hipSuccess) return e;
-        kern<<<dim3(blocks_of(w.units, kAtWaves), l.passes), kAtThreads, lds, s>>>(g, b, a, l, w, (T*)out, lse, part);
-    } else {
-        const Walk w = make_walk<false>(B, g.M, l);
-        auto kern = k_at<T, BUF, R, false, false>;
-        if ((e = allow_lds(kern, lds)) != hipSuccess) return e;
-        kern<<<dim3(blocks_of(w.units, kAtWaves), l.passes), kAtThreads, lds, s>>>(g, b, a, l, w, (T*)out, lse, part);
-    }
+template <typename T, bool BUF, int R, bool EACH, bool BLOCK>
+hipError_t forward_with(const Groups& g, int32_t B, const Attn& a, const Bias& b, const Lanes& l, const Partial& part,
+                        void* out, float* lse, hipStream_t s) {
+    const Walk w = make_walk(B, g.M, EACH ? l.S : 1, 1);
+    size_t floats = Chunk::floats(placed(b), Rounds<EACH, kUnroll<R>>::rows_n(l), l.Hc * R);
+    if (BLOCK) floats += (size_t)l.Hc * R * (a.D + 2);
+    const Shape sh = shape_of(b, floats);
+    auto kern = k_at<T, BUF, R, EACH, BLOCK>;
+    hipError_t e = allow_lds(kern, sh.lds);
+    if (e != hipSuccess) return e;
+    kern<<<dim3(blocks_of(w.units, BLOCK ? 1 : sh.waves), l.passes, part.parts), sh.waves * kWave, sh.lds, s>>>(
+        g, b, a, l, w, (T*)out, lse, part);
     if (part.parts > 1) {
         const int64_t n = (int64_t)g.rows * a.H;
         k_at_join<T><<<blocks_of(n, kAtWaves), kAtThreads, 0, s>>>(part, g.rows, a, (T*)out, lse);
@@ -846,11 +1021,27 @@ hipError_t forward_as(const Groups& g, int32_t B, const Attn& a, const Bias& b, 
     return hipGetLastError();
 }
 
+template <typename T, bool BUF, int R>
+hipError_t forward_as(const Groups& g, int32_t B, const Attn& a, const Bias& b, void* out, float* lse, void* ws,
+                      hipStream_t s) {
+    const Lanes l = make_lanes<T>(a.H / R, a.D);
+    const Split sp = split_of(g, a.H * a.D);
+    Partial part = {nullptr, nullptr, sp.parts};
+    if (part.parts > 1) {
+        part.ml = (float*)ws;
+        part.acc = part.ml + (size_t)part.parts * g.rows * a.H * 2;
+    }
+    auto f = sp.block ? forward_with<T, BUF, R, false, true>
+             : each_of(g.rows, g.idx_len, l) ? forward_with<T, BUF, R, true, false>
+                                             : forward_with<T, BUF, R, false, false>;
+    return f(g, B, a, b, l, part, out, lse, s);
+}
+
 template <typename T>
 hipError_t forward(const Groups& g, int32_t B, const Attn& a, const Bias& b, void* out, float* lse, void* ws,
                    hipStream_t s) {
     const bool buf = vectors<T>(g, a, {a.q, a.k, a.v, out});
-    const int r = heads_per_lane(a);
+    const int r = heads_per_lane<T>(a);
     auto f = buf ? (r == 4 ? forward_as<T, true, 4> : r == 2 ? forward_as<T, true, 2> : forward_as<T, true, 1>)
                  : forward_as<T, false, 1>;
     return f(g, B, a, b, out, lse, ws, s);
@@ -859,58 +1050,54 @@ hipError_t forward(const Groups& g, int32_t B, const Attn& a, const Bias& b, voi
 template <typename T, bool BUF, bool EACH>
 hipError_t back_centers(const Groups& g, int32_t B, const Attn& a, const Bias& b, const Lanes& l, const float* lse,
                         const void* dout, void* dq, float2* stat, hipStream_t s) {
-    const Walk w = make_walk<EACH>(B, g.M, l);
-    const size_t lds = (size_t)Score::floats(b) * 4;
+    const Walk w = make_walk(B, g.M, EACH ? l.S : 1, 1);
+    const Shape sh = shape_of(b, Chunk::floats(placed(b), Rounds<EACH, kUnroll<1>>::rows_n(l), l.Hc));
     auto kern = k_at_back_c<T, BUF, EACH>;
-    hipError_t e = allow_lds(kern, lds);
+    hipError_t e = allow_lds(kern, sh.lds);
     if (e != hipSuccess) return e;
-    kern<<<dim3(blocks_of(w.units, kAtWaves), l.passes), kAtThreads, lds, s>>>(g, b, a, l, w, lse, (const T*)dout,
-                                                                              (T*)dq, stat);
+    kern<<<dim3(blocks_of(w.units, sh.waves), l.passes), sh.waves * kWave, sh.lds, s>>>(
+        g, b, a, l, w, lse, (const T*)dout, (T*)dq, stat);
     return hipGetLastError();
 }
 
-// The launch of the gradient at the points: waves of a workgroup whose tables
-// fit its LDS, and the workgroups, each with partial sums of its own.
+// The launch of the gradient at the points. Points are walked in a row by a
+// slot while their lists are short and the places fit 32 bits; several of them
+// where there are enough for three rounds of the card's waves.
 struct BackShape {
-    int waves;
+    bool flat;
+    Walk walk;
+    Shape sh;
     uint32_t blocks;
-    size_t lds;
 };
 
-BackShape back_shape(int64_t units, int32_t passes, const Bias& b, bool tab) {
+BackShape back_shape(const Groups& g, int32_t B, const Attn& a, const Bias& b, const Lanes& l, bool tab) {
     BackShape r;
-    const size_t base = (size_t)Score::floats(b) * 4, entries = (size_t)(3 * b.nb + 1) * b.H * 4;
-    r.waves = kAtWaves;
-    if (!tab) {
-        r.blocks = blocks_of(units, r.waves);
-        r.lds = base;
-        return r;
+    const int64_t points = (int64_t)B * g.N;
+    r.flat = g.idx_len < (1ll << 31) && each_of(points, g.idx_len, l);
+    const int32_t step = l.Hc * l.G, most = step < kPoints ? step : kPoints;
+    const int64_t P = points / ((int64_t)l.S * 12288);
+    r.walk = r.flat ? make_walk(B, g.N, l.S, (int32_t)(P < 1 ? 1 : P > most ? most : P)) : make_walk(B, g.N, 1, 1);
+    const int rows = r.flat ? Rounds<true, kBackUnroll>::rows_n(l) : Rounds<false, kBackUnroll>::rows_n(l);
+    size_t floats = Chunk::floats(placed(b), rows, l.Hc * (a.H / a.Hkv));
+    if (tab) floats += (size_t)(3 * b.nb + 1) * a.H;
+    r.sh = shape_of(b, floats);
+    r.blocks = blocks_of(r.walk.units, r.sh.waves);
+    if (tab) {  // each workgroup writes a table
+        const uint32_t most_b = kAtParts / l.passes;
+        if (r.blocks > most_b) r.blocks = most_b < 8 ? 8 : most_b & ~7u;
     }
-    while (r.waves > 1 && base + entries * r.waves > kAtLds) r.waves >>= 1;
-    r.lds = base + entries * r.waves;
-    r.blocks = blocks_of(units, r.waves);
-    const uint32_t most = kAtParts / passes;
-    if (r.blocks > most) r.blocks = most < 8 ? 8 : most & ~7u;
     return r;
 }
 
-bool points_each(const Groups& g, int32_t B, const Lanes& l) { return each_of((int64_t)B * g.N, g.idx_len, l); }
-
-int64_t point_units(const Groups& g, int32_t B, const Lanes& l) {
-    return points_each(g, B, l) ? make_walk<true>(B, g.N, l).units : make_walk<false>(B, g.N, l).units;
-}
-
-template <typename T, bool BUF, bool EACH, bool TAB>
-hipError_t back_points(const Groups& g, int32_t B, const Attn& a, const Bias& b, const Lanes& l, const int64_t* pt_off,
-                       const int32_t* pt_center, int64_t capacity, const float2* stat, const void* dout, void* dk,
-                       void* dv, float* part, hipStream_t s) {
-    const Walk w = make_walk<EACH>(B, g.N, l);
-    const BackShape r = back_shape(w.units, l.passes, b, TAB);
-    auto kern = k_at_back_p<T, BUF, EACH, TAB>;
-    hipError_t e = allow_lds(kern, r.lds);
+template <typename T, bool BUF, bool FLAT, bool TAB>
+hipError_t back_points(const Groups& g, const Attn& a, const Bias& b, const Lanes& l, const BackShape& r,
+                       const int64_t* pt_off, const int32_t* pt_center, int64_t capacity, const float2* stat,
+                       const void* dout, void* dk, void* dv, float* part, hipStream_t s) {
+    auto kern = k_at_back_p<T, BUF, FLAT, TAB>;
+    hipError_t e = allow_lds(kern, r.sh.lds);
     if (e != hipSuccess) return e;
-    kern<<<dim3(r.blocks, l.passes), r.waves * kWave, r.lds, s>>>(g, b, a, l, w, pt_off, pt_center, capacity, stat,
-                                                                  (const T*)dout, (T*)dk, (T*)dv, part);
+    kern<<<dim3(r.blocks, l.passes), r.sh.waves * kWave, r.sh.lds, s>>>(
+        g, b, a, l, r.walk, pt_off, pt_center, capacity, stat, (const T*)dout, (T*)dk, (T*)dv, part);
     return hipGetLastError();
 }
 
@@ -922,21 +1109,21 @@ hipError_t backward(const Groups& g, int32_t B, const Attn& a, const Bias& b, co
     float2* stat = (float2*)ws;
     float* part = (float*)((char*)ws + align256((size_t)g.rows * a.H * 8));
     const bool buf = vectors<T>(g, a, {a.q, a.k, a.v, dout, dq, dk, dv});
-    const bool ec = each_of(g.rows, g.idx_len, lc), ep = points_each(g, B, lp), tab = dtable || dslope;
+    const bool ec = each_of(g.rows, g.idx_len, lc), tab = dtable || dslope;
     auto fc = buf ? (ec ? back_centers<T, true, true> : back_centers<T, true, false>)
                   : (ec ? back_centers<T, false, true> : back_centers<T, false, false>);
     hipError_t e = fc(g, B, a, b, lc, lse, dout, dq, stat, s);
     if (e != hipSuccess) return e;
+    const BackShape r = back_shape(g, B, a, b, lp, tab);
     auto with = [&](auto bufc, auto tabc) {
         constexpr bool BUF = decltype(bufc)::value, TAB = decltype(tabc)::value;
-        return (ep ? back_points<T, BUF, true, TAB> : back_points<T, BUF, false, TAB>)(
-            g, B, a, b, lp, pt_off, pt_center, capacity, stat, dout, dk, dv, part, s);
+        return (r.flat ? back_points<T, BUF, true, TAB> : back_points<T, BUF, false, TAB>)(
+            g, a, b, lp, r, pt_off, pt_center, capacity, stat, dout, dk, dv, part, s);
     };
     const std::true_type yes;
     const std::false_type no;
     e = buf ? (tab ? with(yes, yes) : with(yes, no)) : (tab ? with(no, yes) : with(no, no));
     if (e != hipSuccess || !tab) return e;
-    const BackShape r = back_shape(point_units(g, B, lp), lp.passes, b, true);
     return launch_bias_reduce(part, (int32_t)r.blocks * lp.passes, b, dtable, dslope, s);
 }
 
@@ -948,13 +1135,13 @@ Lanes lanes_of(int32_t dtype, int32_t heads, int32_t D) {
 
 size_t group_attention_bytes(const Groups& g, int32_t B, const Attn& a, int32_t dtype, const Bias& b, bool backward) {
     if (!backward) {
-        const Split sp = split_of(g, 1, a.H * a.D);
+        const Split sp = split_of(g, a.H * a.D);
         return sp.parts > 1 ? (size_t)sp.parts * g.rows * a.H * (2 + a.D) * 4 : 0;
     }
     const size_t stat = align256((size_t)g.rows * a.H * 8);
-    if (b.nb == 0 && !b.slope) return stat;
+    if (!placed(b)) return stat;
     const Lanes l = lanes_of(dtype, a.Hkv, a.D);
-    const BackShape r = back_shape(point_units(g, B, l), l.passes, b, true);
+    const BackShape r = back_shape(g, B, a, b, l, true);
     return stat + (size_t)r.blocks * l.passes * (3 * b.nb + 1) * b.H * 4;
 }
 

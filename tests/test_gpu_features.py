@@ -97,6 +97,21 @@ def test_attention_forms(dt, cap, nb, slope, form):
     _run(c, dt, 4, 2, 16, nb, slope, cap, 3, f"{form} {dt} {cap} {nb}")
 
 
+@pytest.mark.parametrize("dt,H,Hkv,D,N,M", [(BF16, 2, 2, 32, 40000, 38000), (F32, 4, 2, 16, 24001, 20001),
+                                            (F16, 5, 5, 24, 14000, 13001), (BF16, 1, 1, 8, 270000, 262200),
+                                            (F32, 3, 1, 7, 40001, 29000), (F16, 8, 4, 16, 70000, 20000)])
+def test_attention_many_short_lists(dt, H, Hkv, D, N, M):
+    """So many short lists that each slot of a wave takes its own, at the centers and,
+    walked through in a row, at the points: most of a few entries, many of none, one
+    of hundreds."""
+    rng = np.random.default_rng(N)
+    for K in (3, 0):
+        c = F.rand_groups(rng, 1, N, M, K, masked=0.1, lens=rng.choice([0, 1, 2, 5], M) if K == 0 else None)
+        c.idx[rng.random(c.idx.shape) < 300 / c.idx.size] = 77  # one point in many groups
+        c = F.Case(1, N, M, c.idx, n_valid=c.n_valid, off=c.off, rng=rng)
+        _run(c, dt, H, Hkv, D, 9, True, 4.0, 5, f"{dt} {H} {Hkv} {D} {N} {M} K={K}")
+
+
 def test_attention_long_lists():
     """Few centers with long lists: the work is split along them. Lengths that leave
     later parts empty, an empty list, and one center alone."""
