@@ -35,8 +35,7 @@ namespace {
 
 constexpr int kAtThreads = 256;
 constexpr int kAtWaves = kAtThreads / kWave;
-constexpr int kAtBlocks = 256 * 8;   // workgroups of a launch; they go round where there is more to do
-constexpr int kAtParts = 1024;       // workgroups of the gradient at the points, where the bias wants its own
+constexpr int kAtBlocks = 256 * 3;   // workgroups of a launch; they go round where there is more to do
 constexpr int kAtLds = 144 << 10;    // LDS of a workgroup: edges, table, chunks, and the waves' gradient tables
 constexpr int kTableFloats = 8192;   // largest table that a workgroup copies to LDS
 constexpr int kPoints = 16;          // most points in a row whose lists one slot walks (FLAT)
@@ -112,11 +111,29 @@ struct Rows {
         if constexpr (BUF) return i < 0 ? kNone : (uint32_t)i * row_bytes;
         else return (uint32_t)i;
     }
-    __device__ __forceinline__ Raw load(uint32_t key) const {
-        if constexpr (BUF) return __builtin_amdgcn_raw_buffer_load_b128(rsrc, key + lane_off, 0, 0);
-        else return load_channels<T, false>(base + (int64_t)(int32_t)key * row, (int32_t)key >= 0 ? n : 0);
+    // `elems`: elements further on, the same for the wave.
+    __device__ __forceinline__ Raw load(uint32_t key, int elems = 0) const {
+        if constexpr (BUF)
+            return __builtin_amdgcn_raw_buffer_load_b128(rsrc, key + lane_off, elems * (int)sizeof(T), 0);
+        else return load_channels<T, false>(base + (int64_t)(int32_t)key * row + elems, (int32_t)key >= 0 ? n : 0);
     }
     static __device__ __forceinline__ bool there(uint32_t key) { return (int32_t)key >= 0; }
+};
+
+// Rows to write, dense.
+template <typename T, bool BUF>
+struct RowsOut {
+    T* base;
+    int64_t row;
+    int n;
+
+    __device__ __forceinline__ RowsOut(T* first, int64_t row_, int lane_elem, int n_)
+        : base(first + lane_elem), row(row_), n(n_) {}
+    __device__ __forceinline__ void store(int32_t i, const float (&x)[kVec<T>]) const {
+        if constexpr (BUF)  // a cloud's rows take less than 2^31 bytes
+            store_channels<T, BUF>((T*)((char*)base + (uint32_t)i * (uint32_t)(row * (int)sizeof(T))), n, x);
+        else store_channels<T, BUF>(base + i * row, n, x);
+    }
 };
 
 // What all kernels know of the scores.
@@ -184,10 +201,10 @@ __device__ __forceinline__ float log_sum(float x) { return kLn2 * __builtin_amdg
 // A chunk of a wave's entries in LDS, a row each: the bias of the wave's heads
 // (where there is a bias), then fields. The entries' lanes write the rows and
 // the slots' lanes read them; a wave's own LDS operations run in order. Rows
-// that no entry's lane writes stay without an entry. An index of kMasked is an
-// entry that is passed over, one of kNoEntry none.
-constexpr int32_t kMasked = -1, kNoEntry = -2;
-constexpr int kKey = 0, kKey2 = 1, kIndex = 2, kPlace = 3, kDist = 4, kPoint = 5, kFields = 8;
+// that no entry's lane writes stay without an entry. Fields: the keys of the
+// entry's two rows; at the points also that of its (lse, delta), its point
+// (-1: no entry) and the keys of the point's own rows.
+constexpr int kKey = 0, kKey2 = 1, kStat = 2, kPoint = 3, kPKey = 4, kPKey2 = 5, kPlace = 6, kDist = 7, kFields = 8;
 
 struct Chunk {
     float* rows;
@@ -203,24 +220,25 @@ struct Chunk {
         for (int r = lane_id(); r < rows_n; r += kWave) {
             rows[r * stride + hp + kKey] = __uint_as_float(kNone);
             rows[r * stride + hp + kKey2] = __uint_as_float(kNone);
-            rows[r * stride + hp + kIndex] = __int_as_float(kNoEntry);
+            rows[r * stride + hp + kStat] = 0.0f;  // read at any entry
+            rows[r * stride + hp + kPoint] = __int_as_float(-1);
+            rows[r * stride + hp + kPKey] = __uint_as_float(kNone);
+            rows[r * stride + hp + kPKey2] = __uint_as_float(kNone);
         }
     }
     __device__ __forceinline__ const float* row(int r) const { return rows + r * stride; }
     __device__ __forceinline__ uint32_t field(const float* r, int f) const { return __float_as_uint(r[hp + f]); }
+    __device__ __forceinline__ void set(int r, int f, uint32_t v) { rows[r * stride + hp + f] = __uint_as_float(v); }
 
-    // The lane's entry into row r: the keys of its rows, its index (negative:
-    // none), and the bias of heads h0 .. h0 + n.
-    __device__ __forceinline__ void put(int r, uint32_t key, uint32_t key2, int32_t index, uint32_t u, float d,
-                                        const Score& sc, int h0, int n) {
+    // The lane's entry into row r: the keys of its rows, and the bias of heads h0 .. h0 + n.
+    __device__ __forceinline__ void put(int r, uint32_t key, uint32_t key2, uint32_t u, float d, const Score& sc,
+                                        int h0, int n) {
         float* o = rows + r * stride;
-        o[hp + kKey] = __uint_as_float(key);
-        o[hp + kKey2] = __uint_as_float(key2);
-        o[hp + kIndex] = __int_as_float(index);
-        if (!sc.placed()) return;
-        o[hp + kPlace] = __uint_as_float(u);
+        set(r, kKey, key);
+        set(r, kKey2, key2);
+        if (!sc.placed() || (int32_t)key < 0) return;
+        set(r, kPlace, u);
         o[hp + kDist] = d;
-        if (index < 0) return;
         if (((sc.H | h0 | n) & 3) == 0 && sc.lds_table) {
             typedef float f4 __attribute__((ext_vector_type(4)));
             const f4* t0 = (const f4*)(sc.lds + (u & 255u) * sc.H + h0);
@@ -384,12 +402,12 @@ __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lan
         for (int64_t s0 = beg; EACH ? __any(s0 < end) : s0 < end; s0 += rd.chunk) {
             const int n = end - s0 < rd.chunk ? (int)(end - s0) : rd.chunk;
             const int e = EACH ? at.li : lane;
-            int32_t mine = kNoEntry;
+            int32_t mine = -1;
             uint32_t u = 0;
             float dist = 0.0f;
             if (e < n) {
                 mine = g.idx[s0 + e];
-                if ((uint32_t)mine >= (uint32_t)g.N) mine = kMasked;
+                if ((uint32_t)mine >= (uint32_t)g.N) mine = -1;
                 if (sc.placed() && mine >= 0) {
                     float p[3];
                     load_xyz(g.points, p0 + mine, p);
@@ -397,8 +415,8 @@ __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lan
                 }
             }
             if (!EACH || at.slot < l.S)
-                ck.put(EACH ? rd.first + e : e, Rows<T, BUF>::key(mine, krb), Rows<T, BUF>::key(mine, vrb), mine, u,
-                       dist, sc, hw, hn);
+                ck.put(EACH ? rd.first + e : e, Rows<T, BUF>::key(mine, krb), Rows<T, BUF>::key(mine, vrb), u, dist, sc,
+                       hw, hn);
             __builtin_amdgcn_wave_barrier();
             for (int t = 0; EACH ? __any(t < n) : t < n; t += rd.per) {
                 Raw k[U], v[U];
@@ -611,12 +629,12 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
         for (int64_t s0 = beg; EACH ? __any(s0 < end) : s0 < end; s0 += rd.chunk) {
             const int n = end - s0 < rd.chunk ? (int)(end - s0) : rd.chunk;
             const int e = EACH ? at.li : lane;
-            int32_t mine = kNoEntry;
+            int32_t mine = -1;
             uint32_t u = 0;
             float dist = 0.0f;
             if (e < n) {
                 mine = g.idx[s0 + e];
-                if ((uint32_t)mine >= (uint32_t)g.N) mine = kMasked;
+                if ((uint32_t)mine >= (uint32_t)g.N) mine = -1;
                 if (sc.placed() && mine >= 0) {
                     float p[3];
                     load_xyz(g.points, p0 + mine, p);
@@ -624,8 +642,8 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
                 }
             }
             if (!EACH || at.slot < l.S)
-                ck.put(EACH ? rd.first + e : e, Rows<T, BUF>::key(mine, krb), Rows<T, BUF>::key(mine, vrb), mine, u,
-                       dist, sc, hw, hn);
+                ck.put(EACH ? rd.first + e : e, Rows<T, BUF>::key(mine, krb), Rows<T, BUF>::key(mine, vrb), u, dist, sc,
+                       hw, hn);
             __builtin_amdgcn_wave_barrier();
             for (int t = 0; EACH ? __any(t < n) : t < n; t += rd.per) {
                 Raw k[U], v[U];
@@ -721,6 +739,9 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
     }
     const int step = l.Hc * l.G, slot = at.slot < l.S ? at.slot : 0;
     const uint32_t qrb = (uint32_t)(a.q_row * (int64_t)sizeof(T)), orb = (uint32_t)(a.H * a.D * (int)sizeof(T));
+    const uint32_t krb = (uint32_t)(a.k_row * (int64_t)sizeof(T)), vrb = (uint32_t)(a.v_row * (int64_t)sizeof(T));
+    const uint32_t kbytes = cloud_bytes<T>(g.N, a.k_row, a.Hkv * a.D);
+    const uint32_t vbytes = cloud_bytes<T>(g.N, a.v_row, a.Hkv * a.D);
     const uint32_t qbytes = cloud_bytes<T>(g.M, a.q_row, a.H * a.D);
     const uint32_t gbytes = cloud_bytes<T>(g.M, (int64_t)a.H * a.D, a.H * a.D);
 
@@ -737,12 +758,16 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
         }
         const Rows<T, BUF> qr((const T*)a.q + c0 * a.q_row, a.q_row, qbytes, at.head * Rq * a.D + at.chan, at.n);
         const Rows<T, BUF> gr(dout + c0 * a.H * a.D, (int64_t)a.H * a.D, gbytes, at.head * Rq * a.D + at.chan, at.n);
+        const Rows<T, BUF> kr((const T*)a.k + p0 * a.k_row, a.k_row, kbytes, at.head * a.D + at.chan, at.n);
+        const Rows<T, BUF> vr((const T*)a.v + p0 * a.v_row, a.v_row, vbytes, at.head * a.D + at.chan, at.n);
+        const int64_t kd = (int64_t)a.Hkv * a.D;
+        const RowsOut<T, BUF> dkr(dk + p0 * kd, kd, at.head * a.D + at.chan, at.n);
+        const RowsOut<T, BUF> dvr(dv + p0 * kd, kd, at.head * a.D + at.chan, at.n);
+        const float2* st0 = stat + c0 * a.H;
         auto clip = [&](int64_t x) { return x < 0 ? 0 : x > capacity ? capacity : x; };
         const int64_t beg = clip(pt_off[p0 + i0]);
         int64_t total = clip(pt_off[p0 + i0 + n0]) - beg;
         if (total < 0) total = 0;
-        const int64_t o = ((p0 + i0) * a.Hkv + at.head) * a.D + at.chan;  // of the first point's sums
-        const int64_t by = (int64_t)a.Hkv * a.D;
         float gk[W] = {}, gv[W] = {};
         Raw x, y;
         float p3[3] = {};
@@ -759,26 +784,26 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
             while (__any(none != 0)) {
                 if (none && at.on) {
                     const int32_t k = __ffsll((unsigned long long)none) - 1;
-                    store_channels<T, BUF>(dk + o + k * by, at.n, gk);
-                    store_channels<T, BUF>(dv + o + k * by, at.n, gv);
+                    dkr.store(i0 + k, gk);
+                    dvr.store(i0 + k, gv);
                 }
                 none &= none - 1;
             }
         } else {
-            x = load_channels<T, BUF>((const T*)a.k + (p0 + i0) * a.k_row + at.head * a.D + at.chan, at.n);
-            y = load_channels<T, BUF>((const T*)a.v + (p0 + i0) * a.v_row + at.head * a.D + at.chan, at.n);
+            x = kr.load(Rows<T, BUF>::key(i0, krb));
+            y = vr.load(Rows<T, BUF>::key(i0, vrb));
             if (sc.placed()) load_xyz(g.points, p0 + i0, p3);
         }
         auto write = [&](int32_t k) {
 #pragma unroll
             for (int w = 0; w < W; ++w) gk[w] *= a.scale;
-            store_channels<T, BUF>(dk + o + k * by, at.n, gk);
-            store_channels<T, BUF>(dv + o + k * by, at.n, gv);
+            dkr.store(i0 + k, gk);
+            dvr.store(i0 + k, gv);
         };
         for (int64_t s0 = 0; FLAT ? __any(s0 < total) : s0 < total; s0 += rd.chunk) {
             const int n = total - s0 < rd.chunk ? (int)(total - s0) : rd.chunk;
             const int e = FLAT ? at.li : lane;
-            int32_t mine = kNoEntry, k = 0;
+            int32_t mine = -1, k = 0;
             uint32_t u = 0;
             float dist = 0.0f;
             if (FLAT) {  // the last point whose list starts at or before the entry
@@ -790,7 +815,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
             }
             if (e < n) {
                 mine = pt_center[beg + s0 + e];
-                if ((uint32_t)mine >= (uint32_t)g.M) mine = kMasked;
+                if ((uint32_t)mine >= (uint32_t)g.M) mine = -1;
                 if (sc.placed() && mine >= 0) {
                     float c[3];
                     load_xyz(g.centers, c0 + mine, c);
@@ -800,8 +825,13 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
             }
             if (!FLAT || at.slot < l.S) {
                 const int r = FLAT ? rd.first + e : e;
-                ck.put(r, Rows<T, BUF>::key(mine, qrb), Rows<T, BUF>::key(mine, orb), mine, u, dist, sc, hw, hn);
-                if (FLAT) ck.rows[r * ck.stride + ck.hp + kPoint] = __int_as_float(k);
+                ck.put(r, Rows<T, BUF>::key(mine, qrb), Rows<T, BUF>::key(mine, orb), u, dist, sc, hw, hn);
+                if (BUF) ck.set(r, kStat, mine < 0 ? 0u : (uint32_t)mine * (uint32_t)a.H);
+                if (FLAT) {
+                    ck.set(r, kPoint, e < n ? (uint32_t)k : 0xFFFFFFFFu);
+                    ck.set(r, kPKey, Rows<T, BUF>::key(i0 + k, krb));
+                    ck.set(r, kPKey2, Rows<T, BUF>::key(i0 + k, vrb));
+                }
             }
             __builtin_amdgcn_wave_barrier();
             // Entries one after another, the heads that share a key within each (FLAT: an entry's point must not
@@ -824,26 +854,18 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
                     const int h = at.head * Rq + rr[i];
-                    const uint32_t head_off = BUF ? (uint32_t)(rr[i] * a.D * (int)sizeof(T)) : 0u;
                     const float* r0 = ck.row(at_row[i]);
-                    const int32_t jj = (int32_t)ck.field(r0, kIndex);
-                    there[i] = jj >= 0;
                     const uint32_t key = ck.field(r0, kKey), key2 = ck.field(r0, kKey2);
-                    if constexpr (BUF) {
-                        q[i] = qr.load(key + head_off);
-                        go[i] = gr.load(key2 + head_off);
-                    } else {
-                        const int64_t row = c0 + (there[i] ? jj : 0);
-                        q[i] = load_channels<T, false>((const T*)a.q + row * a.q_row + h * a.D + at.chan, at.n);
-                        go[i] = load_channels<T, false>(dout + (row * a.H + h) * a.D + at.chan, at.n);
-                    }
-                    st[i] = stat[(c0 + (there[i] ? jj : 0)) * a.H + h];
+                    there[i] = Rows<T, BUF>::there(key);
+                    q[i] = qr.load(key, rr[i] * a.D);
+                    go[i] = gr.load(key2, rr[i] * a.D);
+                    if constexpr (BUF) st[i] = st0[ck.field(r0, kStat) + (uint32_t)h];
+                    else st[i] = st0[(int64_t)(there[i] ? (int32_t)key : 0) * a.H + h];
                     pk[i] = 0;
                     if (FLAT) {
-                        pk[i] = jj != kNoEntry ? (int32_t)ck.field(r0, kPoint) : -1;
-                        const int64_t pt = p0 + i0 + (pk[i] > 0 ? pk[i] : 0);
-                        kx[i] = load_channels<T, BUF>((const T*)a.k + pt * a.k_row + at.head * a.D + at.chan, at.n);
-                        vx[i] = load_channels<T, BUF>((const T*)a.v + pt * a.v_row + at.head * a.D + at.chan, at.n);
+                        pk[i] = (int32_t)ck.field(r0, kPoint);
+                        kx[i] = kr.load(ck.field(r0, kPKey));
+                        vx[i] = vr.load(ck.field(r0, kPKey2));
                     } else {
                         kx[i] = x;
                         vx[i] = y;
@@ -889,9 +911,9 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                     if constexpr (TAB) {
                         if (at.chan == 0 && there[i] && at.on) {
                             if (b.nb > 0) {
-                                lds_add(&tab[(pu[i] & 255u) * a.H + h], ds);
-                                lds_add(&tab[(b.nb + (pu[i] >> 8 & 255u)) * a.H + h], ds);
-                                lds_add(&tab[(2 * b.nb + (pu[i] >> 16)) * a.H + h], ds);
+                                lds_add(&tab[__umul24(pu[i] & 255u, (uint32_t)a.H) + h], ds);
+                                lds_add(&tab[__umul24(b.nb + (pu[i] >> 8 & 255u), (uint32_t)a.H) + h], ds);
+                                lds_add(&tab[__umul24(2 * b.nb + (pu[i] >> 16), (uint32_t)a.H) + h], ds);
                             }
                             if (b.slope) lds_add(&tab[3 * b.nb * a.H + h], ds * pd[i]);
                         }
@@ -1082,10 +1104,6 @@ BackShape back_shape(const Groups& g, int32_t B, const Attn& a, const Bias& b, c
     if (tab) floats += (size_t)(3 * b.nb + 1) * a.H;
     r.sh = shape_of(b, floats);
     r.blocks = blocks_of(r.walk.units, r.sh.waves);
-    if (tab) {  // each workgroup writes a table
-        const uint32_t most_b = kAtParts / l.passes;
-        if (r.blocks > most_b) r.blocks = most_b < 8 ? 8 : most_b & ~7u;
-    }
     return r;
 }
 

@@ -137,10 +137,11 @@ __device__ __forceinline__ void store_channels(T* p, int n, const float (&x)[kVe
 #pragma unroll
             for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(x[i]);
         } else {
+            typedef float f32x2 __attribute__((ext_vector_type(2)));
+            typedef T t2 __attribute__((ext_vector_type(2)));
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                r[i] = (uint32_t)__builtin_bit_cast(uint16_t, (T)x[2 * i]) |
-                       (uint32_t)__builtin_bit_cast(uint16_t, (T)x[2 * i + 1]) << 16;
+                r[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[2 * i], x[2 * i + 1]}), t2));
         }
         *reinterpret_cast<u32x4*>(p) = r;
     } else {
