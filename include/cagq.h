@@ -392,7 +392,7 @@ CAGQ_API int cagq_coverage(const cagq_grid* g, const int32_t* node_idx, const in
  * in a group several times. An empty group is allowed.
  *   points  device float [B][N][3] and centers device float [B][M][3]: read
  *           by the calls that take a bias, else may be NULL.
- * 1 <= B, N, M; B*N <= 2^31-1; B*M <= 2^31-1; B*M*K <= 2^40; idx_len <= 2^40.
+ * 1 <= B, N, M; B*N, B*M, B*M*K and idx_len at most 2^31-1.
  */
 typedef struct cagq_groups {
     int32_t B, N, M, K;

@@ -8,7 +8,7 @@ namespace cagq {
 
 namespace {
 
-constexpr int64_t kMaxSlots = 1ll << 40;
+constexpr int64_t kMaxSlots = 2147483647;
 
 bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
