@@ -35,7 +35,12 @@ namespace {
 
 constexpr int kAtThreads = 256;
 constexpr int kAtWaves = kAtThreads / kWave;
-constexpr int kAtBlocks = 256 * 3;   // workgroups of a launch; they go round where there is more to do
+// Workgroups of a launch; they go round where there is more to do. Short lists:
+// as many as the card holds at once, so that the waves of an XCD walk through
+// its rows side by side and none starts late. Long ones: as many as there are,
+// handed out as workgroups end.
+constexpr int kAtBlocks = 256 * 3;
+constexpr int kAtMany = 1 << 16;
 constexpr int kAtLds = 144 << 10;    // LDS of a workgroup: edges, table, chunks, and the waves' gradient tables
 constexpr int kTableFloats = 8192;   // largest table that a workgroup copies to LDS
 constexpr int kPoints = 16;          // most points in a row whose lists one slot walks (FLAT)
@@ -973,8 +978,10 @@ Shape shape_of(const Bias& b, size_t floats_per_wave) {
 
 bool placed(const Bias& b) { return b.nb > 0 || b.slope; }
 
-// A workgroup to a list whose mean length gives each wave a chunk; parts where
-// there are few lists.
+// A workgroup to a list whose mean length gives each wave a chunk, where there
+// are not lists enough to fill the card with a wave each; parts where there
+// are few.
+constexpr int kSplitRows = 4096;
 struct Split {
     bool block;
     int32_t parts;
@@ -983,7 +990,7 @@ struct Split {
 Split split_of(const Groups& g, int32_t HD) {
     Split s = {false, 1};
     const int64_t mean = g.idx_len / g.rows;  // of ragged lists only their mean is known here
-    if (mean < 2 * kWave || HD > kJoinFloats) return s;
+    if (mean < 2 * kWave || HD > kJoinFloats || g.rows >= kSplitRows) return s;
     s.block = true;
     int64_t p = 1024 / g.rows;
     if (p > mean / (2 * kWave)) p = mean / (2 * kWave);
@@ -1013,9 +1020,9 @@ int heads_per_lane(const Attn& a) {
     return 1;
 }
 
-uint32_t blocks_of(int64_t units, int64_t per) {
+uint32_t blocks_of(int64_t units, int64_t per, int64_t most) {
     const int64_t n = (units + per - 1) / per;
-    return (uint32_t)(n > kAtBlocks ? kAtBlocks : n < 8 ? 8 : (n + 7) & ~7ll);
+    return (uint32_t)(n > most ? most : n < 8 ? 8 : (n + 7) & ~7ll);
 }
 
 template <typename K>
@@ -1034,11 +1041,12 @@ hipError_t forward_with(const Groups& g, int32_t B, const Attn& a, const Bias& b
     auto kern = k_at<T, BUF, R, EACH, BLOCK>;
     hipError_t e = allow_lds(kern, sh.lds);
     if (e != hipSuccess) return e;
-    kern<<<dim3(blocks_of(w.units, BLOCK ? 1 : sh.waves), l.passes, part.parts), sh.waves * kWave, sh.lds, s>>>(
+    const uint32_t blocks = blocks_of(w.units, BLOCK ? 1 : sh.waves, EACH ? kAtBlocks : kAtMany);
+    kern<<<dim3(blocks, l.passes, part.parts), sh.waves * kWave, sh.lds, s>>>(
         g, b, a, l, w, (T*)out, lse, part);
     if (part.parts > 1) {
         const int64_t n = (int64_t)g.rows * a.H;
-        k_at_join<T><<<blocks_of(n, kAtWaves), kAtThreads, 0, s>>>(part, g.rows, a, (T*)out, lse);
+        k_at_join<T><<<blocks_of(n, kAtWaves, kAtMany), kAtThreads, 0, s>>>(part, g.rows, a, (T*)out, lse);
     }
     return hipGetLastError();
 }
@@ -1077,7 +1085,7 @@ hipError_t back_centers(const Groups& g, int32_t B, const Attn& a, const Bias& b
     auto kern = k_at_back_c<T, BUF, EACH>;
     hipError_t e = allow_lds(kern, sh.lds);
     if (e != hipSuccess) return e;
-    kern<<<dim3(blocks_of(w.units, sh.waves), l.passes), sh.waves * kWave, sh.lds, s>>>(
+    kern<<<dim3(blocks_of(w.units, sh.waves, EACH ? kAtBlocks : kAtMany), l.passes), sh.waves * kWave, sh.lds, s>>>(
         g, b, a, l, w, lse, (const T*)dout, (T*)dq, stat);
     return hipGetLastError();
 }
@@ -1103,7 +1111,7 @@ BackShape back_shape(const Groups& g, int32_t B, const Attn& a, const Bias& b, c
     size_t floats = Chunk::floats(placed(b), rows, l.Hc * (a.H / a.Hkv));
     if (tab) floats += (size_t)(3 * b.nb + 1) * a.H;
     r.sh = shape_of(b, floats);
-    r.blocks = blocks_of(r.walk.units, r.sh.waves);
+    r.blocks = blocks_of(r.walk.units, r.sh.waves, r.flat || tab ? kAtBlocks : kAtMany);
     return r;
 }
 

@@ -22,8 +22,9 @@ namespace {
 
 constexpr int kPlThreads = 512;
 constexpr int kPlWaves = kPlThreads / kWave;
-constexpr int kPlTile = 4096;       // slots per tile, while that makes at most kPlTiles tiles
-constexpr int kPlTiles = 2048;
+constexpr int kPlTile = 1024;       // slots per tile, while that makes at most kPlTiles tiles
+constexpr int kPlTiles = 512;
+constexpr int kPlRows = 1024;       // ragged: rows of a tile whose starts a workgroup keeps in LDS
 constexpr int kPlBins = 2048;       // most bins
 constexpr int kPlRange = 2048;      // most points of a bin whose counters fit a workgroup's LDS at once
 constexpr int kPlBinSlots = 4096;   // slots a bin should hold (at most 2^shift = kPlRange points for that)
@@ -66,27 +67,38 @@ PlLayout pl_layout(const Groups& g, int32_t B) {
 
 // The slots [s0, s1) of a tile: their groups' rows.
 struct Tile {
-    int64_t s0, row0;
-    int32_t s1_rows;  // ragged: rows the tile may touch after row0
+    int64_t s0;
+    int32_t row0, rows;   // ragged: rows the tile may touch after row0
+    const int32_t* start; // LDS: where each of them starts, from s0
     Magic by_k;
 
-    // Ragged: the last row of [lo, hi] whose list starts at or before s.
-    static __device__ __forceinline__ int32_t row_of(const Groups& g, int64_t s, int32_t lo, int32_t hi) {
-        while (lo < hi) {
-            const int32_t mid = lo + (hi - lo + 1) / 2;
-            if (g.off[mid] <= s) lo = mid;
-            else hi = mid - 1;
+    // The last row whose list starts at or before s, or row 0: a wave's lanes probe 64 rows at once.
+    static __device__ __forceinline__ int32_t row_of(const Groups& g, int64_t s) {
+        int32_t lo = 0, n = g.rows;
+        while (n > 1) {
+            const int32_t step = (n + kWave - 1) / kWave;
+            const int64_t at = (int64_t)lane_id() * step;
+            const int c = __popcll(__ballot(at < n && g.off[lo + (at < n ? at : 0)] <= s));
+            const int32_t skip = c > 0 ? (c - 1) * step : 0;
+            lo += skip;
+            n = n - skip < step ? n - skip : step;
         }
         return lo;
     }
-    __device__ __forceinline__ Tile(const Groups& g, int64_t s0_, int64_t s1, Magic by_k_) : s0(s0_), by_k(by_k_) {
+    // Every thread of the block; ends with a barrier.
+    __device__ __forceinline__ Tile(const Groups& g, int64_t s0_, int64_t s1, Magic by_k_, int32_t* lds)
+        : s0(s0_), rows(0), start(lds), by_k(by_k_) {
         if (g.K > 0) {
-            row0 = s0 / g.K;
-            s1_rows = 0;
+            row0 = (int32_t)(s0 / g.K);
         } else {
-            row0 = row_of(g, s0, 0, g.rows - 1);
-            s1_rows = row_of(g, s1 - 1, (int32_t)row0, g.rows - 1) - (int32_t)row0;
+            row0 = row_of(g, s0);
+            rows = row_of(g, s1 - 1) - row0;
+            for (int r = threadIdx.x; r <= rows && r < kPlRows; r += kPlThreads) {
+                const int64_t d = g.off[row0 + r] - s0;
+                lds[r] = (int32_t)(d < -1 ? -1 : d > 0x7FFFFFFF ? 0x7FFFFFFF : d);
+            }
         }
+        __syncthreads();
     }
     // Whether slot s counts; its point over the batch and its center.
     __device__ __forceinline__ bool slot(const Groups& g, int64_t s, uint32_t& gp, int32_t& j) const {
@@ -94,11 +106,18 @@ struct Tile {
         const int32_t i = g.idx[s];
         bool ok = (uint32_t)i < (uint32_t)g.N;
         if (g.K > 0) {
-            const uint32_t d = (uint32_t)(s - row0 * g.K), r = udiv(d, by_k);
-            row = (int32_t)(row0 + r);
+            const uint32_t d = (uint32_t)(s - (int64_t)row0 * g.K), r = udiv(d, by_k);
+            row = row0 + (int32_t)r;
             if (g.n_valid) ok = ok && (int32_t)(d - r * (uint32_t)g.K) < g.n_valid[row];
         } else {
-            row = row_of(g, s, (int32_t)row0, (int32_t)row0 + s1_rows);
+            int32_t lo = 0, hi = rows;
+            while (lo < hi) {
+                const int32_t mid = lo + (hi - lo + 1) / 2;
+                const bool before = rows < kPlRows ? start[mid] <= (int32_t)(s - s0) : g.off[row0 + mid] <= s;
+                if (before) lo = mid;
+                else hi = mid - 1;
+            }
+            row = row0 + lo;
             ok = ok && g.off[row] <= s && s < g.off[row + 1];
         }
         const uint32_t b = udiv((uint32_t)row, g.mm);
@@ -111,6 +130,7 @@ struct Tile {
 __global__ __launch_bounds__(kPlThreads) void k_pl_hist(Groups g, PlLayout L, Magic by_k, uint32_t* __restrict__ hist,
                                                         uint64_t* __restrict__ desc) {
     extern __shared__ uint32_t s_cnt[];
+    __shared__ int32_t s_start[kPlRows];
     for (int i = threadIdx.x; i < L.bins; i += kPlThreads) s_cnt[i] = 0;
     for (int64_t i = (int64_t)blockIdx.x * kPlThreads + threadIdx.x; i <= L.scan_tiles;
          i += (int64_t)gridDim.x * kPlThreads)
@@ -119,7 +139,7 @@ __global__ __launch_bounds__(kPlThreads) void k_pl_hist(Groups g, PlLayout L, Ma
     const int64_t s0 = (int64_t)blockIdx.x * L.tile_slots;
     const int64_t s1 = s0 + L.tile_slots < g.idx_len ? s0 + L.tile_slots : g.idx_len;
     if (s0 < s1) {
-        const Tile t(g, s0, s1, by_k);
+        const Tile t(g, s0, s1, by_k, s_start);
         for (int64_t s = s0 + threadIdx.x; s < s1; s += kPlThreads) {
             uint32_t gp;
             int32_t j;
@@ -188,13 +208,13 @@ __global__ __launch_bounds__(kPlThreads) void k_pl_scatter(Groups g, PlLayout L,
                                                            const uint32_t* __restrict__ hist,
                                                            uint2* __restrict__ rec) {
     extern __shared__ uint32_t s_cnt[];  // [wave][bin]
+    __shared__ int32_t s_start[kPlRows];
     const int wave = threadIdx.x / kWave, lane = lane_id();
     const int64_t s0 = (int64_t)blockIdx.x * L.tile_slots;
     const int64_t s1 = s0 + L.tile_slots < g.idx_len ? s0 + L.tile_slots : g.idx_len;
     if (s0 >= s1) return;
     for (int i = threadIdx.x; i < kPlWaves * L.bins; i += kPlThreads) s_cnt[i] = 0;
-    __syncthreads();
-    const Tile t(g, s0, s1, by_k);
+    const Tile t(g, s0, s1, by_k, s_start);
     const int64_t per = L.tile_slots / kPlWaves;
     const int64_t a = s0 + wave * per, b = a + per < s1 ? a + per : s1;
     uint32_t* cnt = s_cnt + wave * L.bins;
