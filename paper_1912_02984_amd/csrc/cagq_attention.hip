@@ -42,7 +42,6 @@ constexpr int kAtWaves = kAtThreads / kWave;
 constexpr int kAtBlocks = 256 * 3;
 constexpr int kAtMany = 1 << 16;
 constexpr int kAtLds = 144 << 10;    // LDS of a workgroup: edges, table, chunks, and the waves' gradient tables
-constexpr int kTableFloats = 8192;   // largest table that a workgroup copies to LDS
 constexpr int kPoints = 16;          // most points in a row whose lists one slot walks (FLAT)
 constexpr int kJoinFloats = 2048;    // H * D up to which a workgroup's waves join their parts in LDS
 constexpr float kNegInf = -__builtin_inff();
@@ -142,45 +141,13 @@ struct RowsOut {
 };
 
 // What all kernels know of the scores.
-struct Score {
-    Edges ed;
-    const float* table;  // [3][nb][H], the caller's
-    const float* lds;    // a copy of it in LDS (lds_table: it takes at most kTableFloats)
-    const float* slope;  // [H], LDS (zeros where there is none)
-    int nb, H;
-    bool dist, lds_table;
-    float mul;   // of a product: scale, or with a cap 2 log2 e scale / cap
+struct Score : PlaceBias {
+    float mul;  // of a product: scale, or with a cap 2 log2 e scale / cap
     float cap;
 
-    // Floats of LDS before the kernel's own (a multiple of 4).
-    static __host__ __device__ int floats(const Bias& b) {
-        if (b.nb == 0 && !b.slope) return 0;
-        const int t = 3 * b.nb * b.H;
-        return ((t <= kTableFloats ? t : 0) + b.H + 3 * edges_size(b.nb) + 3) & ~3;
-    }
-
-    // Every thread of the block; ends with a barrier.
-    __device__ __forceinline__ Score(const Bias& b, const Attn& a, float* s) {
-        nb = b.nb;
-        H = b.H;
-        dist = b.slope != nullptr;
-        cap = a.cap;
+    __device__ __forceinline__ Score(const Bias& b, const Attn& a, float* s) : PlaceBias(b, s), cap(a.cap) {
         mul = cap > 0.0f ? 2.0f * kLog2e * a.scale / cap : a.scale;
-        const int t = 3 * nb * H;
-        lds_table = t <= kTableFloats;
-        table = b.table;
-        lds = s;
-        if (!placed()) return;
-        if (lds_table) {
-            for (int e = threadIdx.x; e < t; e += blockDim.x) s[e] = b.table[e];
-            s += t;
-        }
-        slope = s;
-        for (int e = threadIdx.x; e < H; e += blockDim.x) s[e] = b.slope ? b.slope[e] : 0.0f;
-        ed = stage_edges(b, s + H);
-        __syncthreads();
     }
-    __device__ __forceinline__ bool placed() const { return nb > 0 || dist; }
 
     // cap * tanh(scale * x / cap) as cap - 2 cap / (1 + exp(2 scale x / cap)):
     // off by some 2^-24 of the cap, not of x, which is what differences of
@@ -244,25 +211,10 @@ struct Chunk {
         if (!sc.placed() || (int32_t)key < 0) return;
         set(r, kPlace, u);
         o[hp + kDist] = d;
-        if (((sc.H | h0 | n) & 3) == 0 && sc.lds_table) {
-            typedef float f4 __attribute__((ext_vector_type(4)));
-            const f4* t0 = (const f4*)(sc.lds + (u & 255u) * sc.H + h0);
-            const f4* t1 = (const f4*)(sc.lds + (sc.nb + (u >> 8 & 255u)) * sc.H + h0);
-            const f4* t2 = (const f4*)(sc.lds + (2 * sc.nb + (u >> 16)) * sc.H + h0);
-            for (int h = 0; h < n / 4; ++h) {
-                f4 b = d * ((const f4*)(sc.slope + h0))[h];
-                if (sc.nb > 0) b += t0[h] + t1[h] + t2[h];
-                ((f4*)o)[h] = b;
-            }
+        if ((h0 & 3) == 0) {
+            for (int h = 0; h < n; h += 4) *(f32x4*)(o + h) = sc.four(u, d, h0 + h);
         } else {
-            const float* t0 = sc.table + (u & 255u) * sc.H + h0;
-            const float* t1 = sc.table + (sc.nb + (u >> 8 & 255u)) * sc.H + h0;
-            const float* t2 = sc.table + (2 * sc.nb + (u >> 16)) * sc.H + h0;
-            for (int h = 0; h < n; ++h) {
-                float b = d * sc.slope[h0 + h];
-                if (sc.nb > 0) b += t0[h] + t1[h] + t2[h];
-                o[h] = b;
-            }
+            for (int h = 0; h < n; ++h) o[h] = sc.one(u, d, h0 + h);
         }
     }
 };
@@ -400,18 +352,20 @@ __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lan
         if (EACH && !live_row) end = beg;
         if (!EACH && (BLOCK || part.parts > 1)) {
             const int split = BLOCK ? waves_b * part.parts : part.parts;
-            const int64_t per = (end - beg + split - 1) / split;
+            int64_t per = (end - beg + split - 1) / split;
+            per = (per + kWave - 1) & -(int64_t)kWave;  // whole chunks
             beg += (BLOCK ? (int64_t)blockIdx.z * waves_b + wave : (int64_t)blockIdx.z) * per;
             end = end < beg + per ? end : beg + per;
         }
+        const int e = EACH ? at.li : lane;
+        int32_t next = beg + e < end ? g.idx[beg + e] : -1;  // of the next chunk
         for (int64_t s0 = beg; EACH ? __any(s0 < end) : s0 < end; s0 += rd.chunk) {
             const int n = end - s0 < rd.chunk ? (int)(end - s0) : rd.chunk;
-            const int e = EACH ? at.li : lane;
-            int32_t mine = -1;
+            int32_t mine = next;
             uint32_t u = 0;
             float dist = 0.0f;
+            next = s0 + rd.chunk + e < end ? g.idx[s0 + rd.chunk + e] : -1;
             if (e < n) {
-                mine = g.idx[s0 + e];
                 if ((uint32_t)mine >= (uint32_t)g.N) mine = -1;
                 if (sc.placed() && mine >= 0) {
                     float p[3];
@@ -631,14 +585,15 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
         int64_t beg, end;
         g.range((int32_t)row, beg, end);
         if (EACH && !live_row) end = beg;
+        const int e = EACH ? at.li : lane;
+        int32_t next = beg + e < end ? g.idx[beg + e] : -1;  // of the next chunk
         for (int64_t s0 = beg; EACH ? __any(s0 < end) : s0 < end; s0 += rd.chunk) {
             const int n = end - s0 < rd.chunk ? (int)(end - s0) : rd.chunk;
-            const int e = EACH ? at.li : lane;
-            int32_t mine = -1;
+            int32_t mine = next;
             uint32_t u = 0;
             float dist = 0.0f;
+            next = s0 + rd.chunk + e < end ? g.idx[s0 + rd.chunk + e] : -1;
             if (e < n) {
-                mine = g.idx[s0 + e];
                 if ((uint32_t)mine >= (uint32_t)g.N) mine = -1;
                 if (sc.placed() && mine >= 0) {
                     float p[3];

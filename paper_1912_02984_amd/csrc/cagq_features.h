@@ -230,18 +230,84 @@ __device__ __forceinline__ void pair_place(const Edges& ed, bool want_dist, cons
     dist = want_dist ? sqrtf((dx * dx + dy * dy) + dz * dz) : 0.0f;
 }
 
-// Bias of head h at a place. `table`: [3][nb][H].
-__device__ __forceinline__ float bias_at(const float* table, int nb, int H, float slope, int h, uint32_t u,
-                                         float dist) {
-    float b = 0.0f;
-    if (nb > 0) {
-        const float x = table[(u & 255u) * H + h];
-        const float y = table[(nb + (u >> 8 & 255u)) * H + h];
-        const float z = table[(2 * nb + (u >> 16)) * H + h];
-        b = x + y + z;
+constexpr int kTableFloats = 8192;  // largest table that a workgroup copies to LDS
+
+// The bias as a workgroup holds it: edges and slopes in LDS, the table as well
+// where it takes at most kTableFloats, its rows rounded up to four heads, so
+// that a lane reads four at once.
+struct PlaceBias {
+    Edges ed;
+    const float* table;  // [3][nb][H], the caller's
+    const float* lds;    // [3][nb][Hp] (lds_table)
+    const float* slope;  // [Hp], zeros where there is none
+    int nb, H, Hp;
+    bool dist, lds_table;
+
+    // Floats of LDS it takes (a multiple of 4). with_table false: places alone.
+    static __host__ __device__ int floats(const Bias& b, bool with_table = true) {
+        if (b.nb == 0 && !b.slope) return 0;
+        const int hp = (b.H + 3) & ~3, t = with_table ? 3 * b.nb * hp : 0;
+        return ((t <= kTableFloats ? t : 0) + hp + 3 * edges_size(b.nb) + 3) & ~3;
     }
-    return fmaf(slope, dist, b);
-}
+
+    // Every thread of the block; ends with a barrier. `s`: 16-byte aligned.
+    __device__ __forceinline__ PlaceBias(const Bias& b, float* s, bool with_table = true) {
+        nb = b.nb;
+        H = b.H;
+        Hp = (H + 3) & ~3;
+        dist = b.slope != nullptr;
+        const int t = with_table ? 3 * nb * Hp : 0;
+        lds_table = t <= kTableFloats;
+        table = b.table;
+        lds = s;
+        if (!placed()) return;
+        if (lds_table) {
+            if (Hp == H) {
+                for (int e = threadIdx.x; e < t; e += blockDim.x) s[e] = b.table[e];
+            } else {
+                for (int e = threadIdx.x; e < t; e += blockDim.x) {
+                    const int r = e / Hp, h = e - r * Hp;
+                    s[e] = h < H ? b.table[r * H + h] : 0.0f;
+                }
+            }
+            s += t;
+        }
+        slope = s;
+        for (int e = threadIdx.x; e < Hp; e += blockDim.x) s[e] = b.slope && e < H ? b.slope[e] : 0.0f;
+        ed = stage_edges(b, s + Hp);
+        __syncthreads();
+    }
+    __device__ __forceinline__ bool placed() const { return nb > 0 || dist; }
+
+    __device__ __forceinline__ uint32_t x_row(uint32_t u) const { return u & 255u; }
+    __device__ __forceinline__ uint32_t y_row(uint32_t u) const { return nb + (u >> 8 & 255u); }
+    __device__ __forceinline__ uint32_t z_row(uint32_t u) const { return 2 * nb + (u >> 16); }
+
+    // Bias of head h at a place.
+    __device__ __forceinline__ float one(uint32_t u, float d, int h) const {
+        float b = slope[h] * d;
+        if (nb == 0) return b;
+        if (lds_table)
+            return b + ((lds[x_row(u) * Hp + h] + lds[y_row(u) * Hp + h]) + lds[z_row(u) * Hp + h]);
+        return b + ((table[x_row(u) * H + h] + table[y_row(u) * H + h]) + table[z_row(u) * H + h]);
+    }
+    // Of heads h to h + 3 (h a multiple of 4).
+    __device__ __forceinline__ f32x4 four(uint32_t u, float d, int h) const {
+        f32x4 b = *(const f32x4*)(slope + h);
+        b *= d;
+        if (nb == 0) return b;
+        if (lds_table) {
+            const f32x4 x = *(const f32x4*)(lds + __umul24(x_row(u), (uint32_t)Hp) + h);
+            const f32x4 y = *(const f32x4*)(lds + __umul24(y_row(u), (uint32_t)Hp) + h);
+            const f32x4 z = *(const f32x4*)(lds + __umul24(z_row(u), (uint32_t)Hp) + h);
+            return b + ((x + y) + z);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (h + i < H) b[i] = one(u, d, h + i);
+        return b;
+    }
+};
 
 __device__ __forceinline__ void load_xyz(const float* p, int64_t i, float (&x)[3]) {
     x[0] = p[3 * i];

@@ -258,6 +258,34 @@ def test_relative_bias(dt, H, nb, slope):
         F.check(got, want, f"{dt} {H} {nb}")
 
 
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+def test_relative_bias_of_what_is_not_finite(dt):
+    """Infinity and NaN in the gradient of slots that count reach their own buckets and
+    heads alone, those of slots that do not count none."""
+    rng = np.random.default_rng(53)
+    c = F.rand_groups(rng, 2, 40, 30, 12, masked=0.1)
+    H = 5
+    bias = F.rand_bias(rng, H, 20, True)
+    dbias = _features(rng, (2, 30, 12, H), dt)
+    flat = dbias.reshape(-1, H)
+    out = np.setdiff1d(np.arange(c.idx.size), c.slot)
+    flat[torch.from_numpy(out)] = float("nan")
+    flat[int(c.slot[3]), 1] = float("inf")
+    flat[int(c.slot[50]), 4] = float("nan")
+    clean = torch.where(torch.isfinite(flat), flat, 0.0).reshape(dbias.shape)
+    want = F.relative_bias(c, bias, clean.to(dt), dt)
+    u, _ = c.places(bias[1])
+    for slot, h, x in ((3, 1, float("inf")), (50, 4, float("nan"))):
+        for a in range(3):
+            want["dtable"][0][a, u[slot, a], h] = x
+        want["dslope"][0][h] = x
+    dtable, dslope = cagq.relative_bias_backward(c.groups(cagq, DEV), _bias(bias), dbias.to(DEV))
+    for got, (ref, bound) in ((dtable, want["dtable"]), (dslope, want["dslope"])):
+        got = got.cpu().double()
+        assert torch.equal(torch.isnan(got), torch.isnan(ref))
+        F.check(dict(x=torch.nan_to_num(got, 0.0, 7.0)), dict(x=(torch.nan_to_num(ref, 0.0, 7.0), bound)), str(dt))
+
+
 def test_relative_bias_outside_ragged_groups():
     """Entries before the first list and behind the last are no group's: 0, and not in the gradient."""
     rng = np.random.default_rng(31)
