@@ -164,6 +164,10 @@ struct Score : PlaceBias {
     __device__ __forceinline__ float slack(float e) const { return cap > 0.0f ? 4.0f * e * (1.0f - e) : 1.0f; }
 };
 
+// Keeps the compiler from making a branch that is hardly ever taken into
+// selects that always run.
+__device__ __forceinline__ void rare() { asm volatile(""); }
+
 // exp(x) of a difference of scores.
 __device__ __forceinline__ float weight(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
@@ -182,12 +186,14 @@ struct Chunk {
     float* rows;
     int hp, stride;
 
+    // Floats of a row: an odd number of groups of four, so that rows one after another start on different banks.
+    static __host__ __device__ int row_floats(int hp) { return (hp + kFields) | 4; }
     static __host__ __device__ int floats(bool placed, int rows_n, int hp) {
-        return rows_n * ((placed ? (hp + 3) & ~3 : 0) + kFields);
+        return rows_n * row_floats(placed ? (hp + 3) & ~3 : 0);
     }
     __device__ __forceinline__ Chunk(float* lds, int rows_n, const Score& sc, int hp_) {
         hp = sc.placed() ? (hp_ + 3) & ~3 : 0;
-        stride = hp + kFields;
+        stride = row_floats(hp);
         rows = lds + (threadIdx.x / kWave) * rows_n * stride;
         for (int r = lane_id(); r < rows_n; r += kWave) {
             rows[r * stride + hp + kKey] = __uint_as_float(kNone);
@@ -277,17 +283,16 @@ struct Rounds {
     static __host__ __device__ int slot_rows(const Lanes& l) { return (l.Hc * l.G + U - 1) / U * U; }
     static __host__ __device__ int rows_n(const Lanes& l) {
         if (EACH) return l.S * slot_rows(l);
-        const int per = U * l.S;
-        return (kWave + per - 1) / per * per;
+        return U * l.S < kWave ? kWave : U * l.S;
     }
     int chunk, first, by, per;  // entries; the slot's first row; from one of the U rows to the next; a round's entries
 
     __device__ __forceinline__ Rounds(const Lanes& l, int slot) {
         const int s = slot < l.S ? slot : 0;
-        chunk = EACH ? l.Hc * l.G : kWave;
         first = EACH ? s * slot_rows(l) : s;
         by = EACH ? 1 : l.S;
         per = EACH ? U : U * l.S;
+        chunk = EACH ? l.Hc * l.G : per < kWave ? kWave / per * per : kWave;  // of whole rounds
     }
 };
 
@@ -313,6 +318,11 @@ __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lan
                                                    float* __restrict__ lse, Partial part) {
     constexpr int W = kVec<T>;
     constexpr int U = kUnroll<R>;
+    struct Round {
+        Raw k[U], v[U];
+        float bias[U * R];
+        bool there[U];
+    };
     extern __shared__ __align__(16) float s_lds[];
     const Score sc(b, a, s_lds);
     const int lane = lane_id(), wave = threadIdx.x / kWave, waves_b = blockDim.x / kWave;
@@ -353,7 +363,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lan
         if (!EACH && (BLOCK || part.parts > 1)) {
             const int split = BLOCK ? waves_b * part.parts : part.parts;
             int64_t per = (end - beg + split - 1) / split;
-            per = (per + kWave - 1) & -(int64_t)kWave;  // whole chunks
+            per = (per + rd.per - 1) / rd.per * rd.per;  // whole rounds
             beg += (BLOCK ? (int64_t)blockIdx.z * waves_b + wave : (int64_t)blockIdx.z) * per;
             end = end < beg + per ? end : beg + per;
         }
@@ -373,42 +383,50 @@ __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lan
                     pair_place(sc.ed, sc.dist, p, c, u, dist);
                 }
             }
-            if (!EACH || at.slot < l.S)
+            if (EACH ? at.slot < l.S : e < rd.chunk)
                 ck.put(EACH ? rd.first + e : e, Rows<T, BUF>::key(mine, krb), Rows<T, BUF>::key(mine, vrb), u, dist, sc,
                        hw, hn);
             __builtin_amdgcn_wave_barrier();
-            for (int t = 0; EACH ? __any(t < n) : t < n; t += rd.per) {
-                Raw k[U], v[U];
-                float s[U * R], bi[U * R];
-                bool there[U];
+            auto load = [&](Round& x, int t) {
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
                     const float* r0 = ck.row(rd.first + t + i * rd.by);
                     const uint32_t key = ck.field(r0, kKey);
-                    there[i] = Rows<T, BUF>::there(key);
-                    k[i] = kr.load(key);
-                    v[i] = vr.load(ck.field(r0, kKey2));
+                    x.there[i] = Rows<T, BUF>::there(key);
+                    x.k[i] = kr.load(key);
+                    x.v[i] = vr.load(ck.field(r0, kKey2));
 #pragma unroll
-                    for (int r = 0; r < R; ++r) bi[i * R + r] = sc.placed() ? r0[hl + r] : 0.0f;
+                    for (int r = 0; r < R; ++r) x.bias[i * R + r] = sc.placed() ? r0[hl + r] : 0.0f;
                 }
+            };
+            auto add = [&](Round& x) {
+                float s[U * R];
 #pragma unroll
                 for (int i = 0; i < U; ++i)
 #pragma unroll
-                    for (int r = 0; r < R; ++r) s[i * R + r] = dot<T>(q[r], k[i]);
+                    for (int r = 0; r < R; ++r) s[i * R + r] = dot<T>(q[r], x.k[i]);
                 group_sums(s, l.G);
+                float low = 0.0f;
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
                         float e2;
-                        const float x = sc.product(s[i * R + r], e2) + bi[i * R + r];
-                        // masked by the bias: whatever k and v hold
-                        const bool off = bi[i * R + r] == kNegInf || !there[i];
-                        if (R == 1 && __any(off && there[i])) {
-                            if (off) v[i] = Raw{0, 0, 0, 0};
-                        }
-                        s[i * R + r] = off ? kNegInf : x;
+                        const float sx = sc.product(s[i * R + r], e2) + x.bias[i * R + r];
+                        s[i * R + r] = x.there[i] ? sx : kNegInf;
+                        low = fminf(low, x.bias[i * R + r]);
                     }
+                }
+                if (__any(low == kNegInf)) {  // masked by the bias: whatever k and v hold
+                    rare();
+#pragma unroll
+                    for (int i = 0; i < U; ++i)
+#pragma unroll
+                        for (int r = 0; r < R; ++r)
+                            if (x.bias[i * R + r] == kNegInf) {
+                                s[i * R + r] = kNegInf;
+                                if (R == 1) x.v[i] = Raw{0, 0, 0, 0};
+                            }
                 }
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
@@ -426,16 +444,21 @@ __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lan
                         const float p = weight(s[i * R + r] - z);
                         sum[r] += p;
                         if (R == 1) {
-                            add_channels<T>(acc[r], p, v[i]);
+                            add_channels<T>(acc[r], p, x.v[i]);
                         } else {
                             // heads of their own biases share v: a masked one passes it over
                             const bool off = s[i * R + r] == kNegInf;
 #pragma unroll
                             for (int w = 0; w < W; ++w)
-                                acc[r][w] = fmaf(p, off ? 0.0f : channel<T>(v[i], w), acc[r][w]);
+                                acc[r][w] = fmaf(p, off ? 0.0f : channel<T>(x.v[i], w), acc[r][w]);
                         }
                     }
                 }
+            };
+            for (int t = 0; EACH ? __any(t < n) : t < n; t += rd.per) {
+                Round x;
+                load(x, t);
+                add(x);
             }
             __builtin_amdgcn_wave_barrier();
         }
@@ -528,10 +551,14 @@ __global__ __launch_bounds__(kAtThreads) void k_at_join(Partial part, int64_t ro
         float sum[1] = {ps * f};
         group_sums(sum, kWave);
         for (int d = lane; d < ((a.D + kWave - 1) & -kWave); d += kWave) {
+            const float* at = part.acc + rh * a.D + (d < a.D ? d : 0);
             float x = 0.0f;
-            for (int p = 0; p < part.parts; ++p) {
-                const float fp = __shfl(f, p, kWave);
-                if (d < a.D && fp > 0.0f) x = fmaf(part.acc[(p * all_rh + rh) * a.D + d], fp, x);
+            for (int p = 0; p < part.parts; p += 8) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = p + i < part.parts ? at[(int64_t)(p + i) * all_rh * a.D] : 0.0f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x = fmaf(v[i], __shfl(f, (p + i) & 63, kWave), x);
             }
             if (d < a.D) out[rh * a.D + d] = (T)(sum[0] == 0.0f ? 0.0f : x / sum[0]);
         }
@@ -601,7 +628,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
                     pair_place(sc.ed, sc.dist, p, c, u, dist);
                 }
             }
-            if (!EACH || at.slot < l.S)
+            if (EACH ? at.slot < l.S : e < rd.chunk)
                 ck.put(EACH ? rd.first + e : e, Rows<T, BUF>::key(mine, krb), Rows<T, BUF>::key(mine, vrb), u, dist, sc,
                        hw, hn);
             __builtin_amdgcn_wave_barrier();
@@ -629,6 +656,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
                     float e2 = 0.0f, dp = s[2 * i + 1];
                     float x = sc.product(s[2 * i], e2) + bi[i];
                     if (__any(bi[i] == kNegInf)) {  // masked by the bias: whatever k and v hold
+                        rare();
                         if (bi[i] == kNegInf) {
                             k[i] = Raw{0, 0, 0, 0};
                             x = kNegInf;
@@ -783,7 +811,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                     pair_place(sc.ed, sc.dist, p3, c, u, dist);
                 }
             }
-            if (!FLAT || at.slot < l.S) {
+            if (FLAT ? at.slot < l.S : e < rd.chunk) {
                 const int r = FLAT ? rd.first + e : e;
                 ck.put(r, Rows<T, BUF>::key(mine, qrb), Rows<T, BUF>::key(mine, orb), u, dist, sc, hw, hn);
                 if (BUF) ck.set(r, kStat, mine < 0 ? 0u : (uint32_t)mine * (uint32_t)a.H);
@@ -846,6 +874,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                     float e2 = 0.0f, dp = s[2 * i + 1];
                     float v = sc.product(s[2 * i], e2) + bi[i];
                     if (__any(bi[i] == kNegInf)) {
+                        rare();
                         if (bi[i] == kNegInf) {
                             q[i] = go[i] = Raw{0, 0, 0, 0};
                             v = kNegInf;
@@ -948,7 +977,7 @@ Split split_of(const Groups& g, int32_t HD) {
     if (mean < 2 * kWave || HD > kJoinFloats || g.rows >= kSplitRows) return s;
     s.block = true;
     int64_t p = 1024 / g.rows;
-    if (p > mean / (2 * kWave)) p = mean / (2 * kWave);
+    if (p > mean / kWave) p = mean / kWave;  // 16 entries to a wave
     s.parts = (int32_t)(p < 1 ? 1 : p > kWave ? kWave : p);
     return s;
 }
