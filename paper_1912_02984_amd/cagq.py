@@ -458,27 +458,33 @@ MAX_HEADS = 128
 MAX_HEAD_DIM = 256
 
 
+_F32, _I32, _I64, _U8 = torch.float32, torch.int32, torch.int64, torch.uint8
+
+
 def _on(t: torch.Tensor, dtype, shape, name: str, dev):
     """A contiguous tensor on ``dev``."""
-    if t.dtype != dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
         raise ValueError(f"{name}: expected contiguous {dtype} {tuple(shape)} on {dev}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
-def _empty(shape, dtype, dev, stream):
+def _empty(like: torch.Tensor, shape, dtype, stream):
     """A tensor whose memory is handed on in the order of the stream it is used on."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _workspace(workspace: Optional[torch.Tensor], need: int, dev, stream):
+def _workspace(workspace: Optional[torch.Tensor], need: int, like: torch.Tensor, stream):
+    """The workspace (or None), its address and size."""
     if workspace is None:
-        return _empty(need, torch.uint8, dev, stream) if need else None
-    if workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
-        raise ValueError(f"workspace: expected contiguous torch.uint8 on {dev}")
-    return workspace
+        if not need:
+            return None, None, 0
+        workspace = _empty(like, need, _U8, stream)
+    elif workspace.dtype is not _U8 or workspace.device != like.device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: expected contiguous torch.uint8 on {like.device}")
+    return workspace, workspace.data_ptr(), workspace.numel()
 
 
 class Groups:
@@ -498,27 +504,29 @@ class Groups:
         cur = _cur_device() if _cur_device is not None else torch.cuda.current_device()
         if dev.index != cur:
             raise ValueError(f"groups on {dev}, but the current device is cuda:{cur}")
-        B, N, M = points.shape[0], points.shape[1], centers.shape[1]
-        _on(points, torch.float32, (B, N, 3), "points", dev)
-        _on(centers, torch.float32, (B, M, 3), "centers", dev)
-        K = 0
+        B, N, _ = points.shape
+        M = centers.shape[1]
+        _on(points, _F32, (B, N, 3), "points", dev)
+        _on(centers, _F32, (B, M, 3), "centers", dev)
+        K, nv, of = 0, None, None
         if off is None:
             if idx.dim() != 3 or idx.shape[2] < 1:
                 raise ValueError("idx must be [B, M, K], or off be given")
-            K = idx.shape[2]
-            _on(idx, torch.int32, (B, M, K), "idx", dev)
+            K, entries = idx.shape[2], 0
+            _on(idx, _I32, (B, M, K), "idx", dev)
             if n_valid is not None:
-                _on(n_valid, torch.int32, (B, M), "n_valid", dev)
+                _on(n_valid, _I32, (B, M), "n_valid", dev)
+                nv = n_valid.data_ptr()
         else:
             if n_valid is not None or idx.dim() != 1:
                 raise ValueError("ragged groups have idx [entries] and no n_valid")
-            _on(idx, torch.int32, idx.shape, "idx", dev)
-            _on(off, torch.int64, (B * M + 1,), "off", dev)
+            entries = idx.shape[0]
+            _on(idx, _I32, (entries,), "idx", dev)
+            _on(off, _I64, (B * M + 1,), "off", dev)
+            of = off.data_ptr()
         self.idx, self.points, self.centers, self.n_valid, self.off = idx, points, centers, n_valid, off
         self.B, self.N, self.M, self.K, self.device = B, N, M, K, dev
-        self.rec = GroupsC(B, N, M, K, idx.data_ptr(), None if n_valid is None else n_valid.data_ptr(),
-                           None if off is None else off.data_ptr(), 0 if K else idx.numel(), points.data_ptr(),
-                           centers.data_ptr())
+        self.rec = GroupsC(B, N, M, K, idx.data_ptr(), nv, of, entries, points.data_ptr(), centers.data_ptr())
 
     @property
     def slots(self) -> int:
@@ -541,13 +549,13 @@ class RelativeBias:
             nb = table.shape[1] if table.dim() == 3 else 0
             if not 1 <= nb <= MAX_BUCKETS:
                 raise ValueError(f"table must be [3, buckets, H] with 1 to {MAX_BUCKETS} buckets")
-            _on(table, torch.float32, (3, nb, H), "table", dev)
+            _on(table, _F32, (3, nb, H), "table", dev)
             if edges is None and nb > 1:
                 raise ValueError("a table needs edges [3, buckets - 1]")
         if edges is not None:
-            _on(edges, torch.float32, (3, max(0, nb - 1)), "edges", dev)
+            _on(edges, _F32, (3, max(0, nb - 1)), "edges", dev)
         if slope is not None:
-            _on(slope, torch.float32, (H,), "slope", dev)
+            _on(slope, _F32, (H,), "slope", dev)
         self.table, self.edges, self.slope, self.H, self.device = table, edges, slope, H, dev
         self.rec = BiasC(None if table is None else table.data_ptr(), None if edges is None else edges.data_ptr(),
                          None if slope is None else slope.data_ptr(), nb)
@@ -556,10 +564,12 @@ class RelativeBias:
 def _feature_rows(t: torch.Tensor, B: int, n: int, dtype, name: str, dev) -> int:
     """Elements from one row of ``t`` [B, n, heads, D] to the next; its heads and channels are contiguous, its
     rows evenly spaced (a part of a larger projection, say)."""
-    if t.dim() != 4 or t.shape[0] != B or t.shape[1] != n or t.dtype != dtype or t.device != dev:
+    if t.dim() != 4 or t.dtype is not dtype or t.device != dev or t.shape[:2] != (B, n):
         raise ValueError(f"{name}: expected {dtype} [{B}, {n}, heads, D] on {dev}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     _, _, h, d = t.shape
+    if t.is_contiguous():
+        return h * d
     sb, sn, sh, sd = t.stride()
     row = sn if n > 1 else sb if B > 1 else h * d
     if (d > 1 and sd != 1) or (h > 1 and sh != d) or (B > 1 and sb != n * row) or row < h * d:
@@ -570,17 +580,19 @@ def _feature_rows(t: torch.Tensor, B: int, n: int, dtype, name: str, dev) -> int
 
 def _attn(groups: Groups, q, k, v, bias: Optional[RelativeBias], scale, cap):
     dev, dtype = groups.device, q.dtype
-    if dtype not in FEATURES:
+    code = FEATURES.get(dtype)
+    if code is None:
         raise ValueError(f"q: features are {', '.join(str(x) for x in FEATURES)}, got {dtype}")
     qr = _feature_rows(q, groups.B, groups.M, dtype, "q", dev)
     kr = _feature_rows(k, groups.B, groups.N, dtype, "k", dev)
     vr = _feature_rows(v, groups.B, groups.N, dtype, "v", dev)
-    H, D, Hkv = q.shape[2], q.shape[3], k.shape[2]
-    if v.shape != k.shape or k.shape[3] != D or Hkv < 1 or H % Hkv:
+    _, _, H, D = q.shape
+    _, _, Hkv, Dk = k.shape
+    if v.shape != k.shape or Dk != D or Hkv < 1 or H % Hkv:
         raise ValueError(f"heads of q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not fit")
     if bias is not None and (bias.H != H or bias.device != dev):
         raise ValueError(f"bias: expected {H} heads on {dev}, got {bias.H} on {bias.device}")
-    return AttnC(FEATURES[dtype], H, Hkv, D, D ** -0.5 if scale is None else scale, cap, qr, kr, vr)
+    return AttnC(code, H, Hkv, D, D ** -0.5 if scale is None else scale, cap, qr, kr, vr)
 
 
 def group_attention(groups: Groups, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -593,21 +605,19 @@ def group_attention(groups: Groups, q: torch.Tensor, k: torch.Tensor, v: torch.T
     a = _attn(groups, q, k, v, bias, scale, cap)
     dev = groups.device
     if out is None:
-        out = _empty((groups.B, groups.M, a.H, a.D), q.dtype, dev, stream)
+        out = _empty(q, q.shape, q.dtype, stream)
     else:
-        _on(out, q.dtype, (groups.B, groups.M, a.H, a.D), "out", dev)
+        _on(out, q.dtype, q.shape, "out", dev)
     if lse is None:
-        lse = _empty((groups.B, groups.M, a.H), torch.float32, dev, stream)
+        lse = _empty(q, q.shape[:3], _F32, stream)
     else:
-        _on(lse, torch.float32, (groups.B, groups.M, a.H), "lse", dev)
-    b = None if bias is None else C.byref(bias.rec)
-    need = C.c_size_t()
-    _check(lib().cagq_group_attention_workspace(C.byref(groups.rec), C.byref(a), b, 0, C.byref(need)),
-           "cagq_group_attention")
-    ws = _workspace(workspace, need.value, dev, stream)
-    _check(lib().cagq_group_attention(C.byref(groups.rec), C.byref(a), b, q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                      out.data_ptr(), lse.data_ptr(), _ptr(ws), 0 if ws is None else ws.numel(),
-                                      _stream_ptr(stream)), "cagq_group_attention")
+        _on(lse, _F32, q.shape[:3], "lse", dev)
+    L, need = _lib or lib(), C.c_size_t()
+    g, ab, b = C.byref(groups.rec), C.byref(a), None if bias is None else C.byref(bias.rec)
+    _check(L.cagq_group_attention_workspace(g, ab, b, 0, C.byref(need)), "cagq_group_attention")
+    ws, wp, wn = _workspace(workspace, need.value, q, stream)
+    _check(L.cagq_group_attention(g, ab, b, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                                  wp, wn, _stream_ptr(stream)), "cagq_group_attention")
     return out, lse
 
 
@@ -617,18 +627,18 @@ def point_lists(groups: Groups, off: Optional[torch.Tensor] = None, center: Opti
     groups hold it, ascending, int32 [slots] (-1 behind the last list)."""
     dev = groups.device
     if off is None:
-        off = _empty(groups.B * groups.N + 1, torch.int64, dev, stream)
+        off = _empty(groups.idx, groups.B * groups.N + 1, _I64, stream)
     else:
-        _on(off, torch.int64, (groups.B * groups.N + 1,), "off", dev)
+        _on(off, _I64, (groups.B * groups.N + 1,), "off", dev)
     if center is None:
-        center = _empty(groups.slots, torch.int32, dev, stream)
+        center = _empty(groups.idx, groups.idx.numel(), _I32, stream)
     else:
-        _on(center, torch.int32, center.shape, "center", dev)
-    need = C.c_size_t()
-    _check(lib().cagq_point_lists_workspace(C.byref(groups.rec), C.byref(need)), "cagq_point_lists")
-    ws = _workspace(workspace, need.value, dev, stream)
-    _check(lib().cagq_point_lists(C.byref(groups.rec), off.data_ptr(), center.data_ptr(), center.numel(), _ptr(ws),
-                                  0 if ws is None else ws.numel(), _stream_ptr(stream)), "cagq_point_lists")
+        _on(center, _I32, center.shape, "center", dev)
+    L, g, need = _lib or lib(), C.byref(groups.rec), C.c_size_t()
+    _check(L.cagq_point_lists_workspace(g, C.byref(need)), "cagq_point_lists")
+    ws, wp, wn = _workspace(workspace, need.value, groups.idx, stream)
+    _check(L.cagq_point_lists(g, off.data_ptr(), center.data_ptr(), center.numel(), wp, wn, _stream_ptr(stream)),
+           "cagq_point_lists")
     return off, center
 
 
@@ -643,29 +653,26 @@ def group_attention_backward(groups: Groups, lists, q: torch.Tensor, k: torch.Te
     a = _attn(groups, q, k, v, bias, scale, cap)
     dev = groups.device
     off, center = lists
-    _on(off, torch.int64, (groups.B * groups.N + 1,), "lists[0]", dev)
-    _on(center, torch.int32, center.shape, "lists[1]", dev)
-    _on(lse, torch.float32, (groups.B, groups.M, a.H), "lse", dev)
-    _on(dout, q.dtype, (groups.B, groups.M, a.H, a.D), "dout", dev)
-    kv = (groups.B, groups.N, a.Hkv, a.D)
-    dq = _empty(tuple(dout.shape), q.dtype, dev, stream)
-    dk, dv = _empty(kv, q.dtype, dev, stream), _empty(kv, q.dtype, dev, stream)
+    _on(off, _I64, (groups.B * groups.N + 1,), "lists[0]", dev)
+    _on(center, _I32, center.shape, "lists[1]", dev)
+    _on(lse, _F32, q.shape[:3], "lse", dev)
+    _on(dout, q.dtype, q.shape, "dout", dev)
+    dq = _empty(q, q.shape, q.dtype, stream)
+    dk, dv = _empty(k, k.shape, q.dtype, stream), _empty(k, k.shape, q.dtype, stream)
     dtable = dslope = b = None
     if bias is not None:
         b = C.byref(bias.rec)
         if bias.table is not None:
-            dtable = _empty(tuple(bias.table.shape), torch.float32, dev, stream)
+            dtable = _empty(bias.table, bias.table.shape, _F32, stream)
         if bias.slope is not None:
-            dslope = _empty((a.H,), torch.float32, dev, stream)
-    need = C.c_size_t()
-    _check(lib().cagq_group_attention_workspace(C.byref(groups.rec), C.byref(a), b, 1, C.byref(need)),
-           "cagq_group_attention_backward")
-    ws = _workspace(workspace, need.value, dev, stream)
-    _check(lib().cagq_group_attention_backward(
-        C.byref(groups.rec), C.byref(a), b, off.data_ptr(), center.data_ptr(), center.numel(), q.data_ptr(),
-        k.data_ptr(), v.data_ptr(), lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-        _ptr(dtable), _ptr(dslope), _ptr(ws), 0 if ws is None else ws.numel(), _stream_ptr(stream)),
-        "cagq_group_attention_backward")
+            dslope = _empty(bias.slope, bias.slope.shape, _F32, stream)
+    L, g, ab, need = _lib or lib(), C.byref(groups.rec), C.byref(a), C.c_size_t()
+    _check(L.cagq_group_attention_workspace(g, ab, b, 1, C.byref(need)), "cagq_group_attention_backward")
+    ws, wp, wn = _workspace(workspace, need.value, q, stream)
+    _check(L.cagq_group_attention_backward(
+        g, ab, b, off.data_ptr(), center.data_ptr(), center.numel(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+        lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(dtable), _ptr(dslope),
+        wp, wn, _stream_ptr(stream)), "cagq_group_attention_backward")
     return dict(dq=dq, dk=dk, dv=dv, dtable=dtable, dslope=dslope)
 
 
@@ -673,15 +680,16 @@ def relative_bias(groups: Groups, bias: RelativeBias, dtype=torch.float32, out: 
                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """The relative position bias of every slot (cagq_relative_bias): [B, M, K, H], or [entries, H] of ragged
     groups; 0 in the slots that do not count."""
-    if dtype not in FEATURES or bias.device != groups.device:
+    code = FEATURES.get(dtype)
+    if code is None or bias.device != groups.device:
         raise ValueError(f"relative_bias: {dtype} with a bias on {bias.device} for groups on {groups.device}")
     shape = tuple(groups.idx.shape) + (bias.H,)
     if out is None:
-        out = _empty(shape, dtype, groups.device, stream)
+        out = _empty(groups.idx, shape, dtype, stream)
     else:
         _on(out, dtype, shape, "out", groups.device)
-    _check(lib().cagq_relative_bias(C.byref(groups.rec), C.byref(bias.rec), bias.H, FEATURES[dtype], out.data_ptr(),
-                                    _stream_ptr(stream)), "cagq_relative_bias")
+    _check((_lib or lib()).cagq_relative_bias(C.byref(groups.rec), C.byref(bias.rec), bias.H, code, out.data_ptr(),
+                                              _stream_ptr(stream)), "cagq_relative_bias")
     return out
 
 
@@ -691,18 +699,17 @@ def relative_bias_backward(groups: Groups, bias: RelativeBias, dbias: torch.Tens
     """(dtable, dslope), float32, for the gradient ``dbias`` of ``relative_bias``'s output
     (cagq_relative_bias_backward); None where the bias has no such part."""
     dev = groups.device
-    if dbias.dtype not in FEATURES or bias.device != dev:
+    code = FEATURES.get(dbias.dtype)
+    if code is None or bias.device != dev:
         raise ValueError(f"relative_bias_backward: {dbias.dtype} with a bias on {bias.device} for groups on {dev}")
     _on(dbias, dbias.dtype, tuple(groups.idx.shape) + (bias.H,), "dbias", dev)
-    dtable = None if bias.table is None else _empty(tuple(bias.table.shape), torch.float32, dev, stream)
-    dslope = None if bias.slope is None else _empty((bias.H,), torch.float32, dev, stream)
-    need = C.c_size_t()
-    _check(lib().cagq_relative_bias_workspace(C.byref(groups.rec), C.byref(bias.rec), bias.H, C.byref(need)),
-           "cagq_relative_bias_backward")
-    ws = _workspace(workspace, need.value, dev, stream)
-    _check(lib().cagq_relative_bias_backward(
-        C.byref(groups.rec), C.byref(bias.rec), bias.H, FEATURES[dbias.dtype], dbias.data_ptr(), _ptr(dtable),
-        _ptr(dslope), _ptr(ws), 0 if ws is None else ws.numel(), _stream_ptr(stream)), "cagq_relative_bias_backward")
+    dtable = None if bias.table is None else _empty(bias.table, bias.table.shape, _F32, stream)
+    dslope = None if bias.slope is None else _empty(bias.slope, bias.slope.shape, _F32, stream)
+    L, g, b, need = _lib or lib(), C.byref(groups.rec), C.byref(bias.rec), C.c_size_t()
+    _check(L.cagq_relative_bias_workspace(g, b, bias.H, C.byref(need)), "cagq_relative_bias_backward")
+    ws, wp, wn = _workspace(workspace, need.value, dbias, stream)
+    _check(L.cagq_relative_bias_backward(g, b, bias.H, code, dbias.data_ptr(), _ptr(dtable), _ptr(dslope), wp, wn,
+                                         _stream_ptr(stream)), "cagq_relative_bias_backward")
     return dtable, dslope
 
 

@@ -127,7 +127,8 @@ __device__ __forceinline__ void add_channels(float (&acc)[kVec<T>], float w, con
 }
 
 // The one rounding to the features' type, to nearest even.
-template <typename T, bool VEC>
+// ONCE: larger than the caches and not read again here.
+template <typename T, bool VEC, bool ONCE = false>
 __device__ __forceinline__ void store_channels(T* p, int n, const float (&x)[kVec<T>]) {
     constexpr int W = kVec<T>;
     if constexpr (VEC) {
@@ -143,7 +144,8 @@ __device__ __forceinline__ void store_channels(T* p, int n, const float (&x)[kVe
             for (int i = 0; i < 4; ++i)
                 r[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[2 * i], x[2 * i + 1]}), t2));
         }
-        *reinterpret_cast<u32x4*>(p) = r;
+        if constexpr (ONCE) __builtin_nontemporal_store(r, reinterpret_cast<u32x4*>(p));
+        else *reinterpret_cast<u32x4*>(p) = r;
     } else {
 #pragma unroll
         for (int i = 0; i < W; ++i)
