@@ -112,6 +112,30 @@ def test_attention_many_short_lists(dt, H, Hkv, D, N, M):
         _run(c, dt, H, Hkv, D, 9, True, 4.0, 5, f"{dt} {H} {Hkv} {D} {N} {M} K={K}")
 
 
+@pytest.mark.parametrize("dt,H,Hkv,D,M", [(BF16, 2, 2, 32, 36000), (F32, 2, 1, 16, 50000), (F16, 8, 8, 32, 9000),
+                                          (F32, 3, 3, 20, 12000)])
+def test_attention_of_tangled_groups(dt, H, Hkv, D, M):
+    """Many groups, some longer than a slot's lanes, the same point two and three
+    times in a group and in all its slots, groups that share all their points,
+    masked slots, points in no group."""
+    rng = np.random.default_rng(M)
+    N = 33000
+    for K in (12, 0):
+        c = F.rand_groups(rng, 1, N, M, K, masked=0.1, lens=rng.choice([0, 1, 3, 9, 70], M, p=[.2, .3, .3, .19, .01])
+                          if K == 0 else None)
+        idx = c.idx.copy()
+        if K:
+            idx[:, ::5, 1] = idx[:, ::5, 0]
+            idx[:, ::7, 3] = idx[:, ::7, 0]
+            idx[:, 1::11] = idx[:, ::11][:, :idx[:, 1::11].shape[1]]
+            idx[:, 5, :] = 4  # one point in all slots
+        else:
+            idx[1::3] = idx[:-1:3]
+        idx[(idx >= 0) & (idx < N)] //= 2  # half of the points in no group
+        c = F.Case(1, N, M, idx, n_valid=c.n_valid, off=c.off, rng=rng)
+        _run(c, dt, H, Hkv, D, 9, True, 4.0, 5, f"{dt} {H} {Hkv} {D} {M} K={K}")
+
+
 def test_attention_long_lists():
     """Few centers with long lists: the work is split along them. Lengths that leave
     later parts empty, an empty list, and one center alone."""
