@@ -437,7 +437,7 @@ typedef struct cagq_bias {
  * point) to the next, heads and channels of a row being contiguous; 0 means
  * densely packed rows. They let q, k and v be parts of one projection.
  * scale multiplies q.k. cap > 0 caps the scaled products: cap * tanh(x / cap);
- * cap = 0 leaves them. 1 <= D <= CAGQ_MAX_HEAD_DIM, 1 <= H <= CAGQ_MAX_HEADS.
+ * cap = 0 leaves them (2 * cap and 3 * scale / cap must be finite). 1 <= D <= CAGQ_MAX_HEAD_DIM, 1 <= H <= CAGQ_MAX_HEADS.
  */
 typedef struct cagq_attn {
     int32_t dtype, H, Hkv, D;
@@ -459,8 +459,9 @@ CAGQ_API int cagq_group_attention_workspace(const cagq_groups* g, const cagq_att
  *   lse   = log(sum_i exp(s_i)),  out = sum_i exp(s_i - lse) * v_i
  * over the slots i of the group. Products, scores, the softmax's maximum and
  * sum and the weighted sum are held in fp32; out is rounded once. A slot whose
- * score is -infinity contributes nothing; a group without any other gives
- * out = 0 and lse = -infinity.
+ * bias is -infinity is masked: it contributes nothing, whatever k and v hold; a
+ * group without any other gives out = 0 and lse = -infinity. Outputs must not
+ * overlap inputs.
  *   q device [B][M][H][D], k and v device [B][N][Hkv][D] (rows q_row, k_row
  *   and v_row apart), out device [B][M][H][D] dense, lse device float
  *   [B][M][H] or NULL; bias may be NULL (none).

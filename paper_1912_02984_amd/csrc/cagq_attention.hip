@@ -44,6 +44,7 @@ constexpr int kAtMany = 1 << 16;
 constexpr int kAtLds = 144 << 10;    // LDS of a workgroup: edges, table, chunks, and the waves' gradient tables
 constexpr int kPoints = 16;          // most points in a row whose lists one slot walks (FLAT)
 constexpr int kJoinFloats = 2048;    // H * D up to which a workgroup's waves join their parts in LDS
+constexpr float kWideCap = 64.0f;    // caps above it: see Score::products
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
@@ -141,33 +142,59 @@ struct RowsOut {
     }
 };
 
-// What all kernels know of the scores.
-struct Score : PlaceBias {
-    float mul;  // of a product: scale, or with a cap 2 log2 e scale / cap
-    float cap;
-
-    __device__ __forceinline__ Score(const Bias& b, const Attn& a, float* s) : PlaceBias(b, s), cap(a.cap) {
-        mul = cap > 0.0f ? 2.0f * kLog2e * a.scale / cap : a.scale;
-    }
-
-    // cap * tanh(scale * x / cap) as cap - 2 cap / (1 + exp(2 scale x / cap)):
-    // off by some 2^-24 of the cap, not of x, which is what differences of
-    // scores call for. `e`: 1 / (1 + exp), of which the tanh's slope is
-    // 4 e (1 - e).
-    __device__ __forceinline__ float product(float x, float& e) const {
-        if (cap > 0.0f) {
-            e = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * mul));
-            return fmaf(-2.0f * cap, e, cap);
-        }
-        return x * mul;
-    }
-    // 1 - tanh^2
-    __device__ __forceinline__ float slack(float e) const { return cap > 0.0f ? 4.0f * e * (1.0f - e) : 1.0f; }
-};
-
 // Keeps the compiler from making a branch that is hardly ever taken into
 // selects that always run.
 __device__ __forceinline__ void rare() { asm volatile(""); }
+
+// What all kernels know of the scores.
+struct Score : PlaceBias {
+    float mul;  // of a product: scale, or with a cap 2 log2 e scale / cap
+    float cap, scale;
+
+    __device__ __forceinline__ Score(const Bias& b, const Attn& a, float* s) : PlaceBias(b, s) {
+        cap = a.cap;
+        scale = a.scale;
+        mul = cap > 0.0f ? 2.0f * kLog2e * a.scale / cap : a.scale;
+    }
+
+    // The scores of N products, s[0], s[BY], ..., before the bias:
+    // cap * tanh(scale * x / cap) as cap - 2 cap / (1 + exp(2 scale x / cap)),
+    // off by some 2^-24 of the cap, not of x. Of a cap above kWideCap that is
+    // too much (a large one stands for hardly any cap), and arguments y below
+    // 1/4 take the series y - y^3/3 + 2y^5/15 - 17y^7/315 + 62y^9/2835, whose
+    // next term is below 2^-26 of it. `e`: 1 / (1 + exp), of which the tanh's
+    // slope is 4 e (1 - e).
+    template <int N, int BY>
+    __device__ __forceinline__ void products(float (&s)[N * BY], float (&e)[N]) const {
+        if (cap > 0.0f) {
+            float x[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                x[i] = s[i * BY];
+                e[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[i] * mul));
+                s[i * BY] = fmaf(-2.0f * cap, e[i], cap);
+            }
+            if (cap > kWideCap) {
+                rare();
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float z = x[i] * scale, y = z / cap, w = y * y;
+                    float p = fmaf(w, 62.0f / 2835.0f, -17.0f / 315.0f);
+                    p = fmaf(w, fmaf(w, fmaf(w, p, 2.0f / 15.0f), -1.0f / 3.0f), 1.0f);
+                    if (fabsf(y) < 0.25f) s[i * BY] = z * p;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                s[i * BY] *= mul;
+                e[i] = 0.5f;  // of a tanh at its steepest
+            }
+        }
+    }
+    // 1 - tanh^2
+    static __device__ __forceinline__ float slack(float e) { return 4.0f * e * (1.0f - e); }
+};
 
 // exp(x) of a difference of scores.
 __device__ __forceinline__ float weight(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
@@ -407,13 +434,13 @@ __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lan
 #pragma unroll
                     for (int r = 0; r < R; ++r) s[i * R + r] = dot<T>(q[r], x.k[i]);
                 group_sums(s, l.G);
-                float low = 0.0f;
+                float low = 0.0f, e2[U * R];
+                sc.template products<U * R, 1>(s, e2);
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
-                        float e2;
-                        const float sx = sc.product(s[i * R + r], e2) + x.bias[i * R + r];
+                        const float sx = s[i * R + r] + x.bias[i * R + r];
                         s[i * R + r] = x.there[i] ? sx : kNegInf;
                         low = fminf(low, x.bias[i * R + r]);
                     }
@@ -652,10 +679,12 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
                     s[2 * i + 1] = dot<T>(go, v[i]);
                 }
                 group_sums(s, l.G);
+                float e2[U];
+                sc.template products<U, 2>(s, e2);
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
-                    float e2 = 0.0f, dp = s[2 * i + 1];
-                    float x = sc.product(s[2 * i], e2) + bi[i];
+                    float dp = s[2 * i + 1];
+                    float x = s[2 * i] + bi[i];
                     if (__any(bi[i] == kNegInf)) {  // masked by the bias: whatever k and v hold
                         rare();
                         if (bi[i] == kNegInf) {
@@ -665,7 +694,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
                         }
                     }
                     const float p = there[i] ? weight(x - z) : 0.0f;
-                    const float pdp = p * dp, sl = sc.slack(e2);
+                    const float pdp = p * dp, sl = Score::slack(e2[i]);
                     sum += pdp;
                     ones += p;
                     add_channels<T>(acc, pdp * sl, k[i]);
@@ -869,11 +898,13 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                     s[2 * i + 1] = dot<T>(go[i], vx[i]);
                 }
                 group_sums(s, l.G);
+                float e2[U];
+                sc.template products<U, 2>(s, e2);
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
                     const int h = at.head * Rq + rr[i];
-                    float e2 = 0.0f, dp = s[2 * i + 1];
-                    float v = sc.product(s[2 * i], e2) + bi[i];
+                    float dp = s[2 * i + 1];
+                    float v = s[2 * i] + bi[i];
                     if (__any(bi[i] == kNegInf)) {
                         rare();
                         if (bi[i] == kNegInf) {
@@ -884,7 +915,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                     }
                     const float p = there[i] ? weight(v - st[i].x) : 0.0f;
                     const float ds = there[i] ? p * (dp - st[i].y) : 0.0f;
-                    const float da = there[i] ? ds * sc.slack(e2) : 0.0f;
+                    const float da = there[i] ? ds * Score::slack(e2[i]) : 0.0f;
                     if (FLAT) {
                         const bool change = pk[i] >= 0 && pk[i] != cur;
                         if (__any(change)) {

@@ -63,6 +63,8 @@ bool make_attn(const cagq_attn* a, Attn* out) {
     if (a->H < 1 || a->H > CAGQ_MAX_HEADS || a->Hkv < 1 || a->H % a->Hkv) return false;
     if (a->D < 1 || a->D > CAGQ_MAX_HEAD_DIM) return false;
     if (!isfinite(a->scale) || !isfinite(a->cap) || a->cap < 0.0f) return false;
+    // what the kernels make of them: twice the cap, and scale / cap to base 2
+    if (a->cap > 0.0f && (!isfinite(2.0f * a->cap) || !isfinite(3.0f * a->scale / a->cap))) return false;
     const int64_t qd = (int64_t)a->H * a->D, kd = (int64_t)a->Hkv * a->D;
     out->q_row = a->q_row ? a->q_row : qd;
     out->k_row = a->k_row ? a->k_row : kd;

@@ -57,7 +57,7 @@ def test_bad_groups_are_refused(bad):
 @pytest.mark.parametrize("bad", [
     dict(dtype=-1), dict(dtype=3), dict(H=0), dict(H=129, Hkv=129), dict(Hkv=0), dict(Hkv=3), dict(Hkv=8), dict(D=0),
     dict(D=257), dict(scale=float("nan")), dict(scale=float("inf")), dict(cap=-1.0), dict(cap=float("nan")),
-    dict(cap=float("inf")), dict(q_row=63), dict(k_row=31), dict(v_row=-32), dict(k_row=1 << 32)])
+    dict(cap=float("inf")), dict(cap=3e38), dict(cap=1e-39), dict(cap=1e-30, scale=1e9), dict(q_row=63), dict(k_row=31), dict(v_row=-32), dict(k_row=1 << 32)])
 def test_bad_attention_shapes_are_refused(bad):
     L, g, a = cagq.lib(), _groups(), _attn(**bad)
     r, n = C.byref, C.c_size_t()

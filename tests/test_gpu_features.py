@@ -74,7 +74,8 @@ def test_point_lists():
 
 @pytest.mark.parametrize("dt", [F32, BF16, F16])
 @pytest.mark.parametrize("H,Hkv,D", [(1, 1, 1), (3, 3, 5), (4, 4, 16), (5, 5, 24), (6, 2, 32), (8, 8, 32), (2, 1, 64),
-                                     (12, 12, 7), (1, 1, 256), (9, 3, 128), (33, 33, 8), (128, 64, 2)])
+                                     (12, 12, 7), (1, 1, 256), (9, 3, 128), (33, 33, 8), (128, 64, 2), (16, 4, 256),
+                                     (128, 1, 8)])
 def test_attention_shapes(dt, H, Hkv, D):
     """Heads and widths: a lane to a head, a wave to a head, several waves to a
     row, odd widths, shared heads; fixed groups with masked slots and a bias."""
@@ -147,6 +148,21 @@ def test_attention_long_lists():
             _run(c, dt, H, Hkv, D, 48, False, 50.0, 5, f"{lens} {dt}")
 
 
+@pytest.mark.parametrize("cap", [1e3, 3e4, 1e6, 1e30])
+def test_attention_wide_caps(cap):
+    """A cap far above the scores is hardly a cap: the score's error goes with the score,
+    not with the cap. Scores stay below 12 in size here, and cap * tanh(x / cap) is
+    within x^3 / (3 cap^2) < 6e-4 of x at the first of these caps, 7e-7 at the second."""
+    rng = np.random.default_rng(3)
+    c = F.rand_groups(rng, 1, 200, 60, 20)
+    q, k, v, dout = (_features(rng, (1, n, 4, 16), F32, 1.4) for n in (60, 200, 200, 60))
+    none = (None, None, None)
+    want = F.attention(c, q, k, v, none, None, cap, dout)
+    for name, (ref, bound) in F.attention(c, q, k, v, none, None, 0.0, dout).items():  # bounds without the cap
+        want[name] = (want[name][0], bound)
+    F.check(_attend(c, q, k, v, none, None, cap, dout), want, f"cap={cap}")
+
+
 def test_attention_masks_and_infinities():
     """-infinity in the bias masks pairs, whole groups among them; the type's lowest
     values and large scores; NaN and infinity where nothing reads: behind
@@ -167,9 +183,14 @@ def test_attention_masks_and_infinities():
         read = read.reshape(B, N)
         k[torch.from_numpy(~read)] = float("nan")
         v[torch.from_numpy(~read)] = float("inf")
+        # a point that only the masked center's groups read holds NaN as well
+        alone = np.setdiff1d(c.pt[c.row % M == 5], c.pt[c.row % M != 5])
+        k.reshape(-1, H, D)[torch.from_numpy(alone)] = float("nan")
+        v.reshape(-1, H, D)[torch.from_numpy(alone)] = float("nan")
         q[0, 3] *= 100.0  # one weight of nearly 1
         bias = (table, edges, None)
-        want = F.attention(c, q, torch.nan_to_num(k, 0.0), torch.nan_to_num(v, posinf=0.0), bias, None, 0.0, dout)
+        want = F.attention(c, q, torch.nan_to_num(k, 0.0), torch.nan_to_num(v, 0.0, posinf=0.0), bias, None, 0.0,
+                           dout)
         got = _attend(c, q, k, v, bias, None, 0.0, dout)
         assert (got["out"][:, 5] == 0).all() and (got["lse"][:, 5] == -np.inf).all()
         assert not read.all() and (got["dk"].cpu()[torch.from_numpy(~read)] == 0).all()
