@@ -28,6 +28,7 @@ constexpr int kPlRows = 1024;       // ragged: rows of a tile whose starts a wor
 constexpr int kPlBins = 2048;       // most bins
 constexpr int kPlRange = 2048;      // most points of a bin whose counters fit a workgroup's LDS at once
 constexpr int kPlBinSlots = 4096;   // slots a bin should hold (at most 2^shift = kPlRange points for that)
+constexpr int kPlKeep = 4;          // slots or entries whose loads a lane has on their way at once
 constexpr int kPlScanItems = 8;
 constexpr int kPlScanTile = kScanThreads * kPlScanItems;
 
@@ -140,10 +141,16 @@ __global__ __launch_bounds__(kPlThreads) void k_pl_hist(Groups g, PlLayout L, Ma
     const int64_t s1 = s0 + L.tile_slots < g.idx_len ? s0 + L.tile_slots : g.idx_len;
     if (s0 < s1) {
         const Tile t(g, s0, s1, by_k, s_start);
-        for (int64_t s = s0 + threadIdx.x; s < s1; s += kPlThreads) {
-            uint32_t gp;
+        for (int64_t s = s0 + threadIdx.x; s < s1; s += kPlKeep * kPlThreads) {
+            uint32_t gp[kPlKeep];
             int32_t j;
-            if (t.slot(g, s, gp, j)) atomicAdd(&s_cnt[gp >> L.shift], 1u);
+            bool on[kPlKeep];
+#pragma unroll
+            for (int i = 0; i < kPlKeep; ++i)
+                on[i] = s + i * kPlThreads < s1 && t.slot(g, s + i * kPlThreads, gp[i], j);
+#pragma unroll
+            for (int i = 0; i < kPlKeep; ++i)
+                if (on[i]) atomicAdd(&s_cnt[gp[i] >> L.shift], 1u);
         }
     }
     __syncthreads();
@@ -218,11 +225,28 @@ __global__ __launch_bounds__(kPlThreads) void k_pl_scatter(Groups g, PlLayout L,
     const int64_t per = L.tile_slots / kPlWaves;
     const int64_t a = s0 + wave * per, b = a + per < s1 ? a + per : s1;
     uint32_t* cnt = s_cnt + wave * L.bins;
-    for (int64_t s = a + lane; s < b; s += kWave) {
-        uint32_t gp;
-        int32_t j;
-        if (t.slot(g, s, gp, j)) atomicAdd(&cnt[gp >> L.shift], 1u);
+    // the wave's first 64 * kPlKeep slots stay in registers
+    uint32_t gp[kPlKeep];
+    int32_t j[kPlKeep];
+    bool on[kPlKeep];
+    auto load = [&](int64_t s) {
+#pragma unroll
+        for (int i = 0; i < kPlKeep; ++i) {
+            gp[i] = 0;
+            j[i] = 0;
+            on[i] = s + i * kWave + lane < b && t.slot(g, s + i * kWave + lane, gp[i], j[i]);
+        }
+    };
+    for (int64_t s = a + kPlKeep * kWave; s < b; s += kPlKeep * kWave) {
+        load(s);
+#pragma unroll
+        for (int i = 0; i < kPlKeep; ++i)
+            if (on[i]) atomicAdd(&cnt[gp[i] >> L.shift], 1u);
     }
+    load(a);
+#pragma unroll
+    for (int i = 0; i < kPlKeep; ++i)
+        if (on[i]) atomicAdd(&cnt[gp[i] >> L.shift], 1u);
     __syncthreads();
     for (int i = threadIdx.x; i < L.bins; i += kPlThreads) {
         uint32_t run = hist[(int64_t)i * L.tiles + blockIdx.x];
@@ -233,12 +257,13 @@ __global__ __launch_bounds__(kPlThreads) void k_pl_scatter(Groups g, PlLayout L,
         }
     }
     __syncthreads();
-    for (int64_t s = a; s < b; s += kWave) {
-        uint32_t gp = 0;
-        int32_t j = 0;
-        const bool on = s + lane < b && t.slot(g, s + lane, gp, j);
-        const uint32_t at = next_place(cnt, on ? gp >> L.shift : 0u, bits, on);
-        if (on) rec[at] = make_uint2(gp, (uint32_t)j);
+    for (int64_t s = a; s < b; s += kPlKeep * kWave) {
+        if (s > a) load(s);
+#pragma unroll
+        for (int i = 0; i < kPlKeep; ++i) {
+            const uint32_t at = next_place(cnt, on[i] ? gp[i] >> L.shift : 0u, bits, on[i]);
+            if (on[i]) rec[at] = make_uint2(gp[i], (uint32_t)j[i]);
+        }
     }
 }
 
@@ -266,9 +291,14 @@ __global__ __launch_bounds__(kPlThreads) void k_pl_build(PlLayout L, const uint3
         uint32_t* cnt = s_cnt + wave * np;
         for (int i = threadIdx.x; i < kPlWaves * np; i += kPlThreads) s_cnt[i] = 0;
         __syncthreads();
-        for (uint32_t e = a + lane; e < b; e += kWave) {
-            const uint32_t k = rec[e].x - (uint32_t)p0;
-            if (k < (uint32_t)np) atomicAdd(&cnt[k], 1u);
+        for (uint32_t e = a + lane; e < b; e += kPlKeep * kWave) {
+            uint32_t k[kPlKeep];
+#pragma unroll
+            for (int i = 0; i < kPlKeep; ++i)
+                k[i] = e + i * kWave < b ? rec[e + i * kWave].x - (uint32_t)p0 : 0xFFFFFFFFu;
+#pragma unroll
+            for (int i = 0; i < kPlKeep; ++i)
+                if (k[i] < (uint32_t)np) atomicAdd(&cnt[k[i]], 1u);
         }
         __syncthreads();
         // each thread's points in a row: their totals, then the prefix over all
@@ -295,13 +325,20 @@ __global__ __launch_bounds__(kPlThreads) void k_pl_build(PlLayout L, const uint3
         }
         done += all;
         __syncthreads();
-        for (uint32_t e = a; e < b; e += kWave) {
-            uint2 r = make_uint2(0, 0);
-            if (e + lane < b) r = rec[e + lane];
-            const uint32_t k = r.x - (uint32_t)p0;
-            const bool on = e + lane < b && k < (uint32_t)np;
-            const uint32_t at = next_place(cnt, on ? k : 0u, bits, on);
-            if (on && at < capacity) center[at] = (int32_t)r.y;
+        for (uint32_t e = a; e < b; e += kPlKeep * kWave) {
+            uint2 r[kPlKeep];
+#pragma unroll
+            for (int i = 0; i < kPlKeep; ++i) {
+                r[i] = make_uint2(0, 0);
+                if (e + i * kWave + lane < b) r[i] = rec[e + i * kWave + lane];
+            }
+#pragma unroll
+            for (int i = 0; i < kPlKeep; ++i) {
+                const uint32_t k = r[i].x - (uint32_t)p0;
+                const bool on = e + i * kWave + lane < b && k < (uint32_t)np;
+                const uint32_t at = next_place(cnt, on ? k : 0u, bits, on);
+                if (on && at < capacity) center[at] = (int32_t)r[i].y;
+            }
         }
         __syncthreads();
     }
