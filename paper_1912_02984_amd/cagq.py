@@ -476,15 +476,31 @@ def _empty(like: torch.Tensor, shape, dtype, stream):
         return like.new_empty(shape, dtype=dtype)
 
 
-def _workspace(workspace: Optional[torch.Tensor], need: int, like: torch.Tensor, stream):
-    """The workspace (or None), its address and size."""
+def _empty_as(like: torch.Tensor, stream):
+    """The same for a dense tensor of the shape and type of ``like``."""
+    if stream is None and like.is_contiguous():
+        return torch.empty_like(like)
+    return _empty(like, like.shape, like.dtype, stream)
+
+
+def _handle(stream: Optional[torch.cuda.Stream]) -> int:
+    if stream is None and _raw_stream is not None and _cur_device is not None:
+        return _raw_stream(_cur_device())
+    return (stream or torch.cuda.current_stream()).cuda_stream
+
+
+def _with_workspace(call, size, workspace: Optional[torch.Tensor], like: torch.Tensor, stream, what: str):
+    """``call(address, bytes)`` with the workspace given, or one of the ``size(pointer)`` that the library asks for."""
     if workspace is None:
-        if not need:
-            return None, None, 0
-        workspace = _empty(like, need, _U8, stream)
+        need = C.c_size_t()
+        _check(size(C.byref(need)), what)
+        if need.value:
+            workspace = _empty(like, need.value, _U8, stream)
     elif workspace.dtype is not _U8 or workspace.device != like.device or not workspace.is_contiguous():
         raise ValueError(f"workspace: expected contiguous torch.uint8 on {like.device}")
-    return workspace, workspace.data_ptr(), workspace.numel()
+    rc = call(None, 0) if workspace is None else call(workspace.data_ptr(), workspace.numel())
+    if rc:
+        raise CagqError(rc, what)
 
 
 class Groups:
@@ -498,21 +514,21 @@ class Groups:
 
     def __init__(self, idx: torch.Tensor, points: torch.Tensor, centers: torch.Tensor,
                  n_valid: Optional[torch.Tensor] = None, off: Optional[torch.Tensor] = None):
-        if points.dim() != 3 or centers.dim() != 3 or not points.is_cuda:
-            raise ValueError("points must be [B, N, 3] and centers [B, M, 3] on the GPU")
         dev = points.device
         cur = _cur_device() if _cur_device is not None else torch.cuda.current_device()
-        if dev.index != cur:
-            raise ValueError(f"groups on {dev}, but the current device is cuda:{cur}")
+        if dev.type != "cuda" or dev.index != cur:
+            raise ValueError(f"points on {dev}, but the current device is cuda:{cur}")
+        if points.dim() != 3 or centers.dim() != 3:
+            raise ValueError("points must be [B, N, 3] and centers [B, M, 3]")
         B, N, _ = points.shape
         M = centers.shape[1]
         _on(points, _F32, (B, N, 3), "points", dev)
         _on(centers, _F32, (B, M, 3), "centers", dev)
-        K, nv, of = 0, None, None
+        K, nv, of, entries = 0, None, None, 0
         if off is None:
             if idx.dim() != 3 or idx.shape[2] < 1:
                 raise ValueError("idx must be [B, M, K], or off be given")
-            K, entries = idx.shape[2], 0
+            K = idx.shape[2]
             _on(idx, _I32, (B, M, K), "idx", dev)
             if n_valid is not None:
                 _on(n_valid, _I32, (B, M), "n_valid", dev)
@@ -545,29 +561,29 @@ class RelativeBias:
         if some is None or not some.is_cuda:
             raise ValueError("a bias needs a table or a slope, on the GPU")
         dev, nb, H = some.device, 0, some.shape[-1] if some.dim() else 0
+        tp = ep = sp = None
         if table is not None:
             nb = table.shape[1] if table.dim() == 3 else 0
             if not 1 <= nb <= MAX_BUCKETS:
                 raise ValueError(f"table must be [3, buckets, H] with 1 to {MAX_BUCKETS} buckets")
             _on(table, _F32, (3, nb, H), "table", dev)
+            tp = table.data_ptr()
             if edges is None and nb > 1:
                 raise ValueError("a table needs edges [3, buckets - 1]")
         if edges is not None:
             _on(edges, _F32, (3, max(0, nb - 1)), "edges", dev)
+            ep = edges.data_ptr()
         if slope is not None:
             _on(slope, _F32, (H,), "slope", dev)
+            sp = slope.data_ptr()
         self.table, self.edges, self.slope, self.H, self.device = table, edges, slope, H, dev
-        self.rec = BiasC(None if table is None else table.data_ptr(), None if edges is None else edges.data_ptr(),
-                         None if slope is None else slope.data_ptr(), nb)
+        self.rec = BiasC(tp, ep, sp, nb)
 
 
-def _feature_rows(t: torch.Tensor, B: int, n: int, dtype, name: str, dev) -> int:
+def _row(t: torch.Tensor, name: str) -> int:
     """Elements from one row of ``t`` [B, n, heads, D] to the next; its heads and channels are contiguous, its
     rows evenly spaced (a part of a larger projection, say)."""
-    if t.dim() != 4 or t.dtype is not dtype or t.device != dev or t.shape[:2] != (B, n):
-        raise ValueError(f"{name}: expected {dtype} [{B}, {n}, heads, D] on {dev}, "
-                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    _, _, h, d = t.shape
+    B, n, h, d = t.shape
     if t.is_contiguous():
         return h * d
     sb, sn, sh, sd = t.stride()
@@ -583,16 +599,17 @@ def _attn(groups: Groups, q, k, v, bias: Optional[RelativeBias], scale, cap):
     code = FEATURES.get(dtype)
     if code is None:
         raise ValueError(f"q: features are {', '.join(str(x) for x in FEATURES)}, got {dtype}")
-    qr = _feature_rows(q, groups.B, groups.M, dtype, "q", dev)
-    kr = _feature_rows(k, groups.B, groups.N, dtype, "k", dev)
-    vr = _feature_rows(v, groups.B, groups.N, dtype, "v", dev)
+    for t, n, name in ((q, groups.M, "q"), (k, groups.N, "k"), (v, groups.N, "v")):
+        if t.dim() != 4 or t.dtype is not dtype or t.device != dev or t.shape[:2] != (groups.B, n):
+            raise ValueError(f"{name}: expected {dtype} [{groups.B}, {n}, heads, D] on {dev}, "
+                             f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     _, _, H, D = q.shape
     _, _, Hkv, Dk = k.shape
     if v.shape != k.shape or Dk != D or Hkv < 1 or H % Hkv:
         raise ValueError(f"heads of q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not fit")
     if bias is not None and (bias.H != H or bias.device != dev):
         raise ValueError(f"bias: expected {H} heads on {dev}, got {bias.H} on {bias.device}")
-    return AttnC(code, H, Hkv, D, D ** -0.5 if scale is None else scale, cap, qr, kr, vr)
+    return AttnC(code, H, Hkv, D, D ** -0.5 if scale is None else scale, cap, _row(q, "q"), _row(k, "k"), _row(v, "v"))
 
 
 def group_attention(groups: Groups, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -603,21 +620,19 @@ def group_attention(groups: Groups, q: torch.Tensor, k: torch.Tensor, v: torch.T
     [B, N, Hkv, D] of float32, bfloat16 or float16. ``scale`` is D ** -0.5 by default; ``cap`` > 0 caps the scores
     by a tanh. Returns (out [B, M, H, D], lse float32 [B, M, H])."""
     a = _attn(groups, q, k, v, bias, scale, cap)
-    dev = groups.device
     if out is None:
-        out = _empty(q, q.shape, q.dtype, stream)
+        out = _empty_as(q, stream)
     else:
-        _on(out, q.dtype, q.shape, "out", dev)
+        _on(out, q.dtype, q.shape, "out", groups.device)
     if lse is None:
         lse = _empty(q, q.shape[:3], _F32, stream)
     else:
-        _on(lse, _F32, q.shape[:3], "lse", dev)
-    L, need = _lib or lib(), C.c_size_t()
-    g, ab, b = C.byref(groups.rec), C.byref(a), None if bias is None else C.byref(bias.rec)
-    _check(L.cagq_group_attention_workspace(g, ab, b, 0, C.byref(need)), "cagq_group_attention")
-    ws, wp, wn = _workspace(workspace, need.value, q, stream)
-    _check(L.cagq_group_attention(g, ab, b, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
-                                  wp, wn, _stream_ptr(stream)), "cagq_group_attention")
+        _on(lse, _F32, q.shape[:3], "lse", groups.device)
+    L, g, ab, b = _lib or lib(), C.byref(groups.rec), C.byref(a), None if bias is None else C.byref(bias.rec)
+    _with_workspace(lambda p, n: L.cagq_group_attention(g, ab, b, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                                        out.data_ptr(), lse.data_ptr(), p, n, _handle(stream)),
+                    lambda need: L.cagq_group_attention_workspace(g, ab, b, 0, need),
+                    workspace, q, stream, "cagq_group_attention")
     return out, lse
 
 
@@ -625,20 +640,19 @@ def point_lists(groups: Groups, off: Optional[torch.Tensor] = None, center: Opti
                 workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """The groups turned round (cagq_point_lists): offsets int64 [B*N + 1] and, for each point, the centers whose
     groups hold it, ascending, int32 [slots] (-1 behind the last list)."""
-    dev = groups.device
+    idx, points = groups.idx, groups.B * groups.N
     if off is None:
-        off = _empty(groups.idx, groups.B * groups.N + 1, _I64, stream)
+        off = _empty(idx, points + 1, _I64, stream)
     else:
-        _on(off, _I64, (groups.B * groups.N + 1,), "off", dev)
+        _on(off, _I64, (points + 1,), "off", groups.device)
     if center is None:
-        center = _empty(groups.idx, groups.idx.numel(), _I32, stream)
+        center = _empty(idx, idx.numel(), _I32, stream)
     else:
-        _on(center, _I32, center.shape, "center", dev)
-    L, g, need = _lib or lib(), C.byref(groups.rec), C.c_size_t()
-    _check(L.cagq_point_lists_workspace(g, C.byref(need)), "cagq_point_lists")
-    ws, wp, wn = _workspace(workspace, need.value, groups.idx, stream)
-    _check(L.cagq_point_lists(g, off.data_ptr(), center.data_ptr(), center.numel(), wp, wn, _stream_ptr(stream)),
-           "cagq_point_lists")
+        _on(center, _I32, center.shape, "center", groups.device)
+    L, g = _lib or lib(), C.byref(groups.rec)
+    _with_workspace(lambda p, n: L.cagq_point_lists(g, off.data_ptr(), center.data_ptr(), center.numel(), p, n,
+                                                    _handle(stream)),
+                    lambda need: L.cagq_point_lists_workspace(g, need), workspace, idx, stream, "cagq_point_lists")
     return off, center
 
 
@@ -657,22 +671,20 @@ def group_attention_backward(groups: Groups, lists, q: torch.Tensor, k: torch.Te
     _on(center, _I32, center.shape, "lists[1]", dev)
     _on(lse, _F32, q.shape[:3], "lse", dev)
     _on(dout, q.dtype, q.shape, "dout", dev)
-    dq = _empty(q, q.shape, q.dtype, stream)
-    dk, dv = _empty(k, k.shape, q.dtype, stream), _empty(k, k.shape, q.dtype, stream)
+    dq, dk, dv = _empty_as(dout, stream), _empty_as(k, stream), _empty_as(k, stream)
     dtable = dslope = b = None
     if bias is not None:
         b = C.byref(bias.rec)
         if bias.table is not None:
-            dtable = _empty(bias.table, bias.table.shape, _F32, stream)
+            dtable = _empty_as(bias.table, stream)
         if bias.slope is not None:
-            dslope = _empty(bias.slope, bias.slope.shape, _F32, stream)
-    L, g, ab, need = _lib or lib(), C.byref(groups.rec), C.byref(a), C.c_size_t()
-    _check(L.cagq_group_attention_workspace(g, ab, b, 1, C.byref(need)), "cagq_group_attention_backward")
-    ws, wp, wn = _workspace(workspace, need.value, q, stream)
-    _check(L.cagq_group_attention_backward(
+            dslope = _empty_as(bias.slope, stream)
+    L, g, ab = _lib or lib(), C.byref(groups.rec), C.byref(a)
+    _with_workspace(lambda p, n: L.cagq_group_attention_backward(
         g, ab, b, off.data_ptr(), center.data_ptr(), center.numel(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-        lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(dtable), _ptr(dslope),
-        wp, wn, _stream_ptr(stream)), "cagq_group_attention_backward")
+        lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(dtable), _ptr(dslope), p, n,
+        _handle(stream)), lambda need: L.cagq_group_attention_workspace(g, ab, b, 1, need),
+        workspace, q, stream, "cagq_group_attention_backward")
     return dict(dq=dq, dk=dk, dv=dv, dtable=dtable, dslope=dslope)
 
 
@@ -683,13 +695,13 @@ def relative_bias(groups: Groups, bias: RelativeBias, dtype=torch.float32, out: 
     code = FEATURES.get(dtype)
     if code is None or bias.device != groups.device:
         raise ValueError(f"relative_bias: {dtype} with a bias on {bias.device} for groups on {groups.device}")
-    shape = tuple(groups.idx.shape) + (bias.H,)
+    shape = (*groups.idx.shape, bias.H)
     if out is None:
         out = _empty(groups.idx, shape, dtype, stream)
     else:
         _on(out, dtype, shape, "out", groups.device)
     _check((_lib or lib()).cagq_relative_bias(C.byref(groups.rec), C.byref(bias.rec), bias.H, code, out.data_ptr(),
-                                              _stream_ptr(stream)), "cagq_relative_bias")
+                                              _handle(stream)), "cagq_relative_bias")
     return out
 
 
@@ -702,14 +714,14 @@ def relative_bias_backward(groups: Groups, bias: RelativeBias, dbias: torch.Tens
     code = FEATURES.get(dbias.dtype)
     if code is None or bias.device != dev:
         raise ValueError(f"relative_bias_backward: {dbias.dtype} with a bias on {bias.device} for groups on {dev}")
-    _on(dbias, dbias.dtype, tuple(groups.idx.shape) + (bias.H,), "dbias", dev)
-    dtable = None if bias.table is None else _empty(bias.table, bias.table.shape, _F32, stream)
-    dslope = None if bias.slope is None else _empty(bias.slope, bias.slope.shape, _F32, stream)
-    L, g, b, need = _lib or lib(), C.byref(groups.rec), C.byref(bias.rec), C.c_size_t()
-    _check(L.cagq_relative_bias_workspace(g, b, bias.H, C.byref(need)), "cagq_relative_bias_backward")
-    ws, wp, wn = _workspace(workspace, need.value, dbias, stream)
-    _check(L.cagq_relative_bias_backward(g, b, bias.H, code, dbias.data_ptr(), _ptr(dtable), _ptr(dslope), wp, wn,
-                                         _stream_ptr(stream)), "cagq_relative_bias_backward")
+    _on(dbias, dbias.dtype, (*groups.idx.shape, bias.H), "dbias", dev)
+    dtable = None if bias.table is None else _empty_as(bias.table, stream)
+    dslope = None if bias.slope is None else _empty_as(bias.slope, stream)
+    L, g, b = _lib or lib(), C.byref(groups.rec), C.byref(bias.rec)
+    _with_workspace(lambda p, n: L.cagq_relative_bias_backward(g, b, bias.H, code, dbias.data_ptr(), _ptr(dtable),
+                                                               _ptr(dslope), p, n, _handle(stream)),
+                    lambda need: L.cagq_relative_bias_workspace(g, b, bias.H, need),
+                    workspace, dbias, stream, "cagq_relative_bias_backward")
     return dtable, dslope
 
 
