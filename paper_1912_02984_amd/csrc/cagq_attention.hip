@@ -24,6 +24,17 @@
 // at the points (dk, dv and the bias's), each recomputing the scores: that
 // reads two rows a pair, as storing and fetching weights for every pair and
 // head would need memory for them all.
+//
+// Measured on indoor scenes (4 x 81920 points, 8192 centers of 32, 8 heads of
+// 32 channels in bfloat16: 779000 pairs, of which each reads two rows of 512
+// bytes): forward 100 us, gradients 112 us at the centers and 250 us at the
+// points. The caches' misses bound all three: 0.57, 0.59 and 1.35 GB at 5.2 to
+// 5.7 TB/s (rows are as much as a cloud's 84 MB apart in time of use, an L2
+// holds 4 MB), against 0.35 GB that the forward cannot do without; its loads
+// without any arithmetic take 97 us. Short rows are bound by issue instead:
+// whole contexts (2 x 3001 centers, 1.28 M pairs, 6 heads of 16) 86 us, of
+// which 45 are vector instructions, the rest of it the longest lists' ends and
+// the L1's 64 lanes' gathers. A few short lists take a chain of cold loads: 8 us.
 #include <initializer_list>
 #include <type_traits>
 
@@ -340,6 +351,8 @@ __device__ __forceinline__ uint32_t cloud_bytes(int32_t rows, int64_t row, int32
 template <int R>
 constexpr int kUnroll = R == 4 ? 2 : 4;
 
+// One pass over a list with the running maximum and sum; what bounds it and what
+// it measured stands at the top.
 // R: query heads a lane holds (they share the key's head).
 template <typename T, bool BUF, int R, bool EACH, bool BLOCK>
 __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lanes l, Walk walk, T* __restrict__ out,
