@@ -16,8 +16,7 @@
 // slots that count, 327680 points): the atomics cross the XCDs' L2s. The four
 // launches here take 36 us (hist 6, scan 6, scatter 11, build 14; 9 MB at the
 // card's copy rate would take 2): latency, each of them two or three dependent
-// loads and a few barriers. Objects (16 x 1024 points, 512 centers of 32) take
-// 22 us, of which the launches' host time is 18.
+// loads and a few barriers.
 #include "cagq_features.h"
 
 namespace cagq {
@@ -36,11 +35,47 @@ constexpr int kPlKeep = 4;          // slots or entries whose loads a lane has o
 constexpr int kPlScanItems = 8;
 constexpr int kPlScanTile = kScanThreads * kPlScanItems;
 
+// Small clouds in one or two launches instead of four: k_pl_cloud takes a range
+// of a cloud's points, reads all of the cloud's slots, keeps those of its
+// points in LDS in slot order, and places them as k_pl_build does. What comes
+// before its range it counts on the way, what the clouds before hold k_pl_total
+// has counted. For clouds whose slots fit its LDS, and batches whose workgroups
+// all run at once. Against the four launches, in a row on a stream: one object
+// (1024 points, 512 centers of 32) 18.9 -> 12.9 us, 16 of them 22.6 -> 16.8, 256
+// of them 80 -> 43; four of 8192 points 23.6 -> 16.8; 64 of 1024 points with 128
+// centers 25 -> 11.
+constexpr int kPcThreads = 1024;
+constexpr int kPcWaves = kPcThreads / kWave;
+constexpr int kPcSlots = 16384;     // most slots of a cloud
+constexpr int kPcWaveSlots = kPcSlots / kPcWaves;
+constexpr int kPcRange = 1024;      // most points of a workgroup
+constexpr int kPcBits = 10;         // of a point within it
+constexpr int kPcAim = 1024;        // slots that its points should have
+constexpr int kPcBlocks = 256;      // most workgroups (their LDS leaves one on a CU)
+constexpr int kPcTotals = 4;        // most parts in which a cloud's slots are counted
+
 struct PlLayout {
     int64_t points;
     int32_t shift, bins, tiles, tile_slots, scan_tiles;
+    int32_t parts, range, totals;  // small clouds: workgroups of a cloud, points of each, counts; otherwise 0
     size_t hist, desc, rec, total;
 };
+
+void small_clouds(const Groups& g, int32_t B, PlLayout& L) {
+    L.parts = L.range = L.totals = 0;
+    const int64_t slots = g.K > 0 ? (int64_t)g.M * g.K : g.idx_len;  // a ragged cloud may have them all
+    if (B < 1 || B > kPcBlocks || g.rows < 1 || g.N < 1 || slots < 1 || slots > kPcSlots || g.M >> (32 - kPcBits))
+        return;
+    int64_t parts = (slots + kPcAim - 1) / kPcAim;
+    if (parts > kPcBlocks / B) parts = kPcBlocks / B;
+    if (parts < (g.N + kPcRange - 1) / kPcRange) parts = (g.N + kPcRange - 1) / kPcRange;
+    const int64_t range = (g.N + parts - 1) / parts;
+    parts = (g.N + range - 1) / range;
+    if (B * parts > kPcBlocks) return;
+    L.parts = (int32_t)parts;
+    L.range = (int32_t)range;
+    L.totals = kPcBlocks / B < kPcTotals ? kPcBlocks / B : kPcTotals;
+}
 
 PlLayout pl_layout(const Groups& g, int32_t B) {
     PlLayout L;
@@ -57,12 +92,18 @@ PlLayout pl_layout(const Groups& g, int32_t B) {
     while ((L.points + (1ll << L.shift) - 1) >> L.shift > kPlBins) ++L.shift;
     L.bins = (int32_t)((L.points + (1ll << L.shift) - 1) >> L.shift);
     L.scan_tiles = (int32_t)(((int64_t)L.bins * L.tiles + kPlScanTile - 1) / kPlScanTile);
+    small_clouds(g, B, L);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
         at = (at + bytes + 255) & ~(size_t)255;
         return here;
     };
+    if (L.parts) {
+        L.hist = take((size_t)B * L.totals * 4);  // slots that count, of each cloud's parts
+        L.total = at;
+        return L;
+    }
     L.hist = take(((size_t)L.bins * L.tiles + 1) * 4);
     L.desc = take(((size_t)L.scan_tiles + 1) * 8);  // look-back descriptors, then the ticket
     L.rec = take((size_t)g.idx_len * 8);
@@ -74,7 +115,7 @@ PlLayout pl_layout(const Groups& g, int32_t B) {
 struct Tile {
     int64_t s0;
     int32_t row0, rows;   // ragged: rows the tile may touch after row0
-    const int32_t* start; // LDS: where each of them starts, from s0
+    const int32_t* start; // LDS: where each of them starts, and the last ends, from s0
     Magic by_k;
 
     // The last row whose list starts at or before s, or row 0: a wave's lanes probe 64 rows at once.
@@ -98,7 +139,7 @@ struct Tile {
         } else {
             row0 = row_of(g, s0);
             rows = row_of(g, s1 - 1) - row0;
-            for (int r = threadIdx.x; r <= rows && r < kPlRows; r += kPlThreads) {
+            for (int r = threadIdx.x; r <= rows + 1 && r <= kPlRows; r += blockDim.x) {
                 const int64_t d = g.off[row0 + r] - s0;
                 lds[r] = (int32_t)(d < -1 ? -1 : d > 0x7FFFFFFF ? 0x7FFFFFFF : d);
             }
@@ -115,15 +156,18 @@ struct Tile {
             row = row0 + (int32_t)r;
             if (g.n_valid) ok = ok && (int32_t)(d - r * (uint32_t)g.K) < g.n_valid[row];
         } else {
-            int32_t lo = 0, hi = rows;
-            while (lo < hi) {
-                const int32_t mid = lo + (hi - lo + 1) / 2;
-                const bool before = rows < kPlRows ? start[mid] <= (int32_t)(s - s0) : g.off[row0 + mid] <= s;
-                if (before) lo = mid;
-                else hi = mid - 1;
-            }
-            row = row0 + lo;
-            ok = ok && g.off[row] <= s && s < g.off[row + 1];
+            const auto search = [&](const auto* from, auto at) {
+                int32_t lo = 0, hi = rows;
+                while (lo < hi) {
+                    const int32_t mid = lo + (hi - lo + 1) / 2;
+                    if (from[mid] <= at) lo = mid;
+                    else hi = mid - 1;
+                }
+                row = row0 + lo;
+                ok = ok && from[lo] <= at && at < from[lo + 1];
+            };
+            if (rows < kPlRows) search(start, (int32_t)(s - s0));
+            else search(g.off + row0, s);
         }
         const uint32_t b = udiv((uint32_t)row, g.mm);
         gp = b * (uint32_t)g.N + (uint32_t)i;
@@ -135,7 +179,7 @@ struct Tile {
 __global__ __launch_bounds__(kPlThreads) void k_pl_hist(Groups g, PlLayout L, Magic by_k, uint32_t* __restrict__ hist,
                                                         uint64_t* __restrict__ desc) {
     extern __shared__ uint32_t s_cnt[];
-    __shared__ int32_t s_start[kPlRows];
+    __shared__ int32_t s_start[kPlRows + 1];
     for (int i = threadIdx.x; i < L.bins; i += kPlThreads) s_cnt[i] = 0;
     for (int64_t i = (int64_t)blockIdx.x * kPlThreads + threadIdx.x; i <= L.scan_tiles;
          i += (int64_t)gridDim.x * kPlThreads)
@@ -219,7 +263,7 @@ __global__ __launch_bounds__(kPlThreads) void k_pl_scatter(Groups g, PlLayout L,
                                                            const uint32_t* __restrict__ hist,
                                                            uint2* __restrict__ rec) {
     extern __shared__ uint32_t s_cnt[];  // [wave][bin]
-    __shared__ int32_t s_start[kPlRows];
+    __shared__ int32_t s_start[kPlRows + 1];
     const int wave = threadIdx.x / kWave, lane = lane_id();
     const int64_t s0 = (int64_t)blockIdx.x * L.tile_slots;
     const int64_t s1 = s0 + L.tile_slots < g.idx_len ? s0 + L.tile_slots : g.idx_len;
@@ -352,6 +396,137 @@ __global__ __launch_bounds__(kPlThreads) void k_pl_build(PlLayout L, const uint3
         center[i] = -1;
 }
 
+// The slots of a cloud, and of one of its waves' part of them.
+__device__ __forceinline__ void cloud_slots(const Groups& g, int32_t b, int64_t& beg, int64_t& end) {
+    int64_t x;
+    g.range(b * g.M, beg, x);
+    g.range(b * g.M + g.M - 1, x, end);
+}
+
+__global__ __launch_bounds__(kPcThreads) void k_pl_total(Groups g, int32_t totals, Magic by_k,
+                                                         uint32_t* __restrict__ total) {
+    __shared__ int32_t s_start[kPlRows + 1];
+    __shared__ uint32_t s_sum[kPcWaves];
+    int64_t beg, end;
+    const int32_t b = (int32_t)blockIdx.x / totals, t0 = (int32_t)blockIdx.x - b * totals;
+    cloud_slots(g, b, beg, end);
+    const int64_t n = end - beg;
+    end = beg + n * (t0 + 1) / totals;
+    beg += n * t0 / totals;
+    uint32_t c = 0;
+    if (beg < end) {
+        const Tile t(g, beg, end, by_k, s_start);
+        for (int64_t s = beg + threadIdx.x; s < end; s += kPlKeep * kPcThreads) {
+#pragma unroll
+            for (int i = 0; i < kPlKeep; ++i) {
+                uint32_t gp;
+                int32_t j;
+                if (s + i * kPcThreads < end) c += t.slot(g, s + i * kPcThreads, gp, j);
+            }
+        }
+    }
+    c = wave_incl_sum_u32(c);
+    if (lane_id() == kWave - 1) s_sum[threadIdx.x / kWave] = c;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        uint32_t all = 0;
+        for (int w = 0; w < kPcWaves; ++w) all += s_sum[w];
+        total[blockIdx.x] = all;
+    }
+}
+
+// total: of the clouds' parts; null: there is one, and its workgroups count all of it.
+__global__ __launch_bounds__(kPcThreads) void k_pl_cloud(Groups g, int32_t B, int32_t parts, int32_t range, Magic by_k,
+                                                         int32_t totals, const uint32_t* __restrict__ total,
+                                                         int64_t* __restrict__ off, int32_t* __restrict__ center,
+                                                         int64_t capacity) {
+    extern __shared__ uint32_t s_dyn[];  // [wave][point] counters, [wave][kPcWaveSlots] (center, point)
+    __shared__ int32_t s_start[kPlRows + 1];
+    __shared__ uint32_t s_sum[kPcWaves], s_base[kPcWaves], s_all[kPcWaves];
+    const int wave = threadIdx.x / kWave, lane = lane_id();
+    const int32_t b = (int32_t)blockIdx.x / parts, p0 = ((int32_t)blockIdx.x - b * parts) * range;
+    const int np = g.N - p0 < range ? g.N - p0 : range;
+    uint32_t* cnt = s_dyn + wave * np;
+    uint32_t* mine = s_dyn + kPcWaves * range + wave * kPcWaveSlots;
+    for (int i = threadIdx.x; i < kPcWaves * np; i += kPcThreads) s_dyn[i] = 0;
+    uint32_t base = 0, all = 0;  // slots before this range; all of the batch
+    if (total)
+        for (int i = threadIdx.x; i < B * totals; i += kPcThreads) {
+            const uint32_t c = total[i];
+            all += c;
+            base += i < b * totals ? c : 0;
+        }
+    int64_t beg, end;
+    cloud_slots(g, b, beg, end);
+    int kept = 0;
+    if (beg < end) {
+        const Tile t(g, beg, end, by_k, s_start);  // with a barrier
+        const int64_t per = ((end - beg + kPcWaves - 1) / kPcWaves + kWave - 1) & ~(int64_t)(kWave - 1);
+        const int64_t a = beg + wave * per, z = a + per < end ? a + per : end;
+        for (int64_t s = a + lane; s - lane < z; s += kPlKeep * kWave) {
+            uint32_t gp[kPlKeep];
+            int32_t j[kPlKeep];
+            bool on[kPlKeep];
+#pragma unroll
+            for (int i = 0; i < kPlKeep; ++i) on[i] = s + i * kWave < z && t.slot(g, s + i * kWave, gp[i], j[i]);
+#pragma unroll
+            for (int i = 0; i < kPlKeep; ++i) {
+                const uint32_t k = gp[i] - ((uint32_t)b * (uint32_t)g.N + (uint32_t)p0);
+                const bool in = on[i] && k < (uint32_t)np;
+                base += on[i] && (int32_t)k < 0;
+                all += !total && on[i];
+                const uint64_t m = __ballot(in);
+                if (in) {
+                    mine[kept + __popcll(m & ((1ull << lane) - 1))] = (uint32_t)j[i] << kPcBits | k;
+                    atomicAdd(&cnt[k], 1u);
+                }
+                kept += __popcll(m);
+            }
+        }
+    }
+    base = wave_incl_sum_u32(base);
+    all = wave_incl_sum_u32(all);
+    if (lane == kWave - 1) {
+        s_base[wave] = base;
+        s_all[wave] = all;
+    }
+    __syncthreads();
+    // a thread's point (at most kPcRange = kPcThreads): its entries, then the prefix over all
+    uint32_t sum = 0;
+    if ((int)threadIdx.x < np)
+        for (int w = 0; w < kPcWaves; ++w) sum += s_dyn[w * np + threadIdx.x];
+    const uint32_t incl = wave_incl_sum_u32(sum);
+    if (lane == kWave - 1) s_sum[wave] = incl;
+    __syncthreads();
+    uint32_t run = incl - sum;
+    all = 0;
+    for (int w = 0; w < kPcWaves; ++w) {
+        run += s_base[w] + (w < wave ? s_sum[w] : 0u);
+        all += s_all[w];
+    }
+    if ((int)threadIdx.x < np) {
+        off[(int64_t)b * g.N + p0 + threadIdx.x] = run;
+        for (int w = 0; w < kPcWaves; ++w) {
+            const uint32_t c = s_dyn[w * np + threadIdx.x];
+            s_dyn[w * np + threadIdx.x] = run;
+            run += c;
+        }
+    }
+    __syncthreads();
+    int bits = 0;
+    while ((1 << bits) < np) ++bits;
+    for (int e = 0; e < kept; e += kWave) {
+        const bool on = e + lane < kept;
+        const uint32_t x = on ? mine[e + lane] : 0u;
+        const uint32_t at = next_place(cnt, x & ((1u << kPcBits) - 1u), bits, on);
+        if (on && at < capacity) center[at] = (int32_t)(x >> kPcBits);
+    }
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) off[(int64_t)B * g.N] = all;
+    for (int64_t i = all + (int64_t)blockIdx.x * kPcThreads + threadIdx.x; i < capacity;
+         i += (int64_t)gridDim.x * kPcThreads)
+        center[i] = -1;
+}
+
 int bits_of(int64_t n) {  // of numbers below n
     int b = 0;
     while ((1ll << b) < n) ++b;
@@ -379,6 +554,14 @@ hipError_t launch_point_lists(const Groups& g, int32_t B, int64_t* pt_off, int32
     const size_t bins_lds = (size_t)L.bins * 4, waves_lds = bins_lds * kPlWaves;
     const size_t range_lds = (size_t)range * 4 * kPlWaves;
     hipError_t e;
+    if (L.parts) {
+        const size_t lds = ((size_t)kPcWaves * L.range + kPcSlots) * 4;
+        if ((e = allow_lds(k_pl_cloud, lds)) != hipSuccess) return e;
+        if (B > 1) k_pl_total<<<B * L.totals, kPcThreads, 0, s>>>(g, L.totals, by_k, hist);
+        k_pl_cloud<<<B * L.parts, kPcThreads, lds, s>>>(g, B, L.parts, L.range, by_k, L.totals,
+                                                        B > 1 ? hist : nullptr, pt_off, pt_center, capacity);
+        return hipGetLastError();
+    }
     if ((e = allow_lds(k_pl_scatter, waves_lds)) != hipSuccess) return e;
     if ((e = allow_lds(k_pl_build, range_lds)) != hipSuccess) return e;
     k_pl_hist<<<L.tiles, kPlThreads, bins_lds, s>>>(g, L, by_k, hist, desc);

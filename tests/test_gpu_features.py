@@ -72,6 +72,51 @@ def test_point_lists():
         assert np.array_equal(center.cpu().numpy(), wcenter), n
 
 
+@pytest.mark.parametrize("B,N,M,K,extra", [
+    (1, 1024, 128, 128, 0), (1, 1024, 5462, 3, 0), (3, 1025, 128, 128, 0), (2, 33, 4097, 4, 0),  # slots of a cloud
+    (256, 10, 3, 4, 0), (257, 10, 3, 4, 0), (255, 1025, 3, 4, 0), (128, 1030, 4, 40, 0),  # clouds
+    (1, 1 << 18, 9, 7, 0), (1, (1 << 18) + 1, 9, 7, 0), (2, 1 << 17, 9, 7, 0),  # points
+    (1, 700, 100, 0, 0), (5, 64, 300, 0, 7), (1, 50, 1, 0, 16383), (1, 50, 1, 0, 16384), (4, 9, 2000, 0, 16384),
+    (1, 5, (1 << 22) - 1, 0, 60), (1, 5, 1 << 22, 0, 60)])  # ragged: entries, centers
+def test_point_lists_at_limits(B, N, M, K, extra):
+    """Sizes on either side of what one workgroup takes of a cloud, and of a
+    launch; every list against a stable sort of the slots that count."""
+    rng = np.random.default_rng(B + N + M + K + extra)
+    rows = B * M
+    if K:
+        idx = rng.integers(-1, N + 1, (rows, K)).astype(np.int32)
+        n = rng.integers(0, K + 1, rows).astype(np.int32)
+        row = np.repeat(np.arange(rows), K)
+        counts = (np.arange(K) < n[:, None]).ravel()
+        form = dict(n_valid=torch.from_numpy(n.reshape(B, M)).to(DEV))
+        shape, flat = (B, M, K), idx.ravel()
+    else:  # few of many groups have entries; `extra` more in the last, and three that no group holds
+        lens = np.where(rng.random(rows) < 500 / rows, rng.integers(0, 9, rows), 0)
+        if M == 1:
+            lens[:] = 0
+        lens[-1] += extra if M == 1 else min(extra, 16384 - int(lens.sum())) if extra > 100 else extra
+        total, tail = int(lens.sum()), 0 if M == 1 else 3
+        flat = rng.integers(-1, N + 1, total + tail).astype(np.int32)
+        row = np.concatenate([np.repeat(np.arange(rows), lens), np.zeros(tail, np.int64)])
+        counts = np.arange(total + tail) < total
+        off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int64)
+        form, shape = dict(off=torch.from_numpy(off).to(DEV)), flat.shape
+    counts &= (flat >= 0) & (flat < N)
+    point, center = (row // M * N + flat)[counts], (row % M)[counts]
+    want = np.full(flat.size, -1, np.int32)
+    want[:center.size] = center[np.argsort(point, kind="stable")]
+    woff = np.concatenate([[0], np.cumsum(np.bincount(point, minlength=B * N))])
+    pts, cen = (torch.zeros((B, m, 3), device=DEV) for m in (N, M))
+    g = cagq.Groups(torch.from_numpy(flat.reshape(shape)).to(DEV), pts, cen, **form)
+    o = torch.full((B * N + 1 + 2,), -7, dtype=torch.int64, device=DEV)
+    c = torch.full((flat.size + 5,), -7, dtype=torch.int32, device=DEV)
+    cagq.point_lists(g, off=o[:-2], center=c[:-2])
+    assert np.array_equal(o[:-2].cpu().numpy(), woff)
+    got = c.cpu().numpy()
+    assert np.array_equal(got[:flat.size], want) and (got[flat.size:-2] == -1).all()
+    assert (got[-2:] == -7).all() and (o[-2:] == -7).all()
+
+
 @pytest.mark.parametrize("dt", [F32, BF16, F16])
 @pytest.mark.parametrize("H,Hkv,D", [(1, 1, 1), (3, 3, 5), (4, 4, 16), (5, 5, 24), (6, 2, 32), (8, 8, 32), (2, 1, 64),
                                      (12, 12, 7), (1, 1, 256), (9, 3, 128), (33, 33, 8), (128, 64, 2), (16, 4, 256),
