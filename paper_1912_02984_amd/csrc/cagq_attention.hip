@@ -982,11 +982,15 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Whether every slot of a wave takes a list of its own: lists short beside a
-// chunk of the slot's lanes, and enough of them.
+// Whether every slot of a wave takes a list of its own: lists short, and the
+// shorter the fewer of them that takes. (Mean lengths of 5 and 8, 5870 and 4542
+// lists: 37 -> 14 and 19 -> 9 us forward; 1, 80 lists: 11 -> 7. Otherwise a wave's
+// slots share a list: 470 ragged ones of 4 on the average 18 us against 30 with
+// one each, 1024 x 8 of 20 in 4 slots with gradients 200 against 207.)
 bool each_of(int64_t rows, int64_t slots, const Lanes& l) {
     if (l.S == 1) return true;
-    return slots / rows <= 32 && rows / l.S >= 4096;
+    const int64_t units = rows / l.S;
+    return slots <= 2 * rows || (slots <= 8 * rows && units >= 64) || (slots <= 32 * rows && units >= 4096);
 }
 
 // The launch of a kernel: waves of a workgroup, such that what they keep in
@@ -1119,9 +1123,20 @@ hipError_t back_centers(const Groups& g, int32_t B, const Attn& a, const Bias& b
     return hipGetLastError();
 }
 
+// Whether a slot walks lists at the points as one, rather than a wave one list
+// after another: while a list does not fill a wave's round, or its rounds are
+// few beside what a wave does once a list. (61341 points with 136 slots 165 -> 28 us,
+// 28264 with 27180 137 -> 44, indoor scenes with gradients, 3 slots a point,
+// 818 -> 369; 23 slots a point in 2 slots 54 -> 49. On the other side 27 slots a
+// point, three query heads to a key's, 4 slots: 340 as lists, 573 as one, in
+// which a wave waits for the longest.)
+bool flat_of(int64_t points, int64_t slots, const Attn& a, const Lanes& l) {
+    return slots < points * 2 * l.S || slots * (a.H / a.Hkv) < points * 32;
+}
+
 // The launch of the gradient at the points. Points are walked in a row by a
-// slot while their lists are short and the places fit 32 bits; several of them
-// where there are enough for three rounds of the card's waves.
+// slot where the places fit 32 bits; several of them where there are enough
+// for more than two rounds of the card's waves (3072 of them).
 struct BackShape {
     bool flat;
     Walk walk;
@@ -1132,9 +1147,9 @@ struct BackShape {
 BackShape back_shape(const Groups& g, int32_t B, const Attn& a, const Bias& b, const Lanes& l, bool tab) {
     BackShape r;
     const int64_t points = (int64_t)B * g.N;
-    r.flat = g.idx_len < (1ll << 31) && each_of(points, g.idx_len, l);
+    r.flat = g.idx_len < (1ll << 31) && flat_of(points, g.idx_len, a, l);
     const int32_t step = l.Hc * l.G, most = step < kPoints ? step : kPoints;
-    const int64_t P = points / ((int64_t)l.S * 12288);
+    const int64_t P = points / ((int64_t)l.S * 8192);
     r.walk = r.flat ? make_walk(B, g.N, l.S, (int32_t)(P < 1 ? 1 : P > most ? most : P)) : make_walk(B, g.N, 1, 1);
     const int rows = r.flat ? Rounds<true, kBackUnroll>::rows_n(l) : Rounds<false, kBackUnroll>::rows_n(l);
     size_t floats = Chunk::floats(placed(b), rows, l.Hc * (a.H / a.Hkv));
