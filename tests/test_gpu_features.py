@@ -182,6 +182,24 @@ def test_attention_of_tangled_groups(dt, H, Hkv, D, M):
         _run(c, dt, H, Hkv, D, 9, True, 4.0, 5, f"{dt} {H} {Hkv} {D} {M} K={K}")
 
 
+@pytest.mark.parametrize("dt,H,Hkv,D,N,M,lens", [
+    (F16, 8, 2, 64, 300, 40, 20), (F32, 4, 1, 16, 300, 40, 20),      # four query heads a lane, a list for all slots
+    (BF16, 2, 2, 5, 6, 300, 40), (F32, 3, 1, 7, 6, 300, 40),         # long lists at the points, rows off 16 bytes
+    (F32, 2, 1, 64, 66000, 400, 3), (F16, 4, 2, 128, 66000, 400, 3),  # several points a slot, shared heads
+    (BF16, 2, 1, 8, 200, 1100, 140), (F32, 1, 1, 3, 200, 1100, 140),  # a workgroup to a list, not cut
+    (F16, 1, 1, 3, 500, 3, 2000), (BF16, 4, 4, 32, 40, 900, 2),      # cut, rows off 16 bytes; a list per slot
+    (F16, 3, 3, 32, 700, 500, 8), (F32, 3, 3, 32, 700, 500, 9)])     # either side of that
+@pytest.mark.parametrize("ragged", [False, True])
+def test_attention_ways_to_share_waves(dt, H, Hkv, D, N, M, lens, ragged):
+    """Every way in which lists share waves, with fixed and ragged groups, with and without a bias."""
+    rng = np.random.default_rng(lens)
+    c = F.rand_groups(rng, 1, N, M, 0 if ragged else lens, masked=0.05, n_valid=M != 1100,
+                      lens=[lens, lens + 1, lens - 1] if ragged else None)
+    _run(c, dt, H, Hkv, D, 5, True, 3.0, 6, f"{dt} {H} {Hkv} {D} {N} {M} {lens} {ragged}")
+    if not ragged:
+        _run(c, dt, H, Hkv, D, 0, False, 0.0, 7, f"{dt} {H} {Hkv} {D} {N} {M} {lens}, no bias")
+
+
 def test_attention_long_lists():
     """Few centers with long lists: the work is split along them. Lengths that leave
     later parts empty, an empty list, and one center alone."""
