@@ -55,7 +55,10 @@ constexpr int kAtMany = 1 << 16;
 constexpr int kAtLds = 144 << 10;    // LDS of a workgroup: edges, table, chunks, and the waves' gradient tables
 constexpr int kPoints = 16;          // most points in a row whose lists one slot walks (FLAT)
 constexpr int kJoinFloats = 2048;    // H * D up to which a workgroup's waves join their parts in LDS
-constexpr float kWideCap = 64.0f;    // caps above it: see Score::products
+// Caps above it: see Score::products. Of 2-byte features a score is off by some
+// 2^-9 of its products' sizes anyway.
+template <typename T>
+constexpr float kWideCap = sizeof(T) == 4 ? 0.0f : 64.0f;
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
@@ -171,11 +174,12 @@ struct Score : PlaceBias {
     // The scores of N products, s[0], s[BY], ..., before the bias:
     // cap * tanh(scale * x / cap) as cap - 2 cap / (1 + exp(2 scale x / cap)),
     // off by some 2^-24 of the cap, not of x. Of a cap above kWideCap that is
-    // too much (a large one stands for hardly any cap), and arguments y below
+    // too much (a large one stands for hardly any cap; float32 features under a
+    // cap of 45 came out 1.3e-6 off instead of 2.2e-7), and arguments y below
     // 1/4 take the series y - y^3/3 + 2y^5/15 - 17y^7/315 + 62y^9/2835, whose
     // next term is below 2^-26 of it. `e`: 1 / (1 + exp), of which the tanh's
     // slope is 4 e (1 - e).
-    template <int N, int BY>
+    template <typename T, int N, int BY>
     __device__ __forceinline__ void products(float (&s)[N * BY], float (&e)[N]) const {
         if (cap > 0.0f) {
             float x[N];
@@ -185,7 +189,7 @@ struct Score : PlaceBias {
                 e[i] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x[i] * mul));
                 s[i * BY] = fmaf(-2.0f * cap, e[i], cap);
             }
-            if (cap > kWideCap) {
+            if (cap > kWideCap<T>) {
                 rare();
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
@@ -448,7 +452,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at(Groups g, Bias b, Attn a, Lan
                     for (int r = 0; r < R; ++r) s[i * R + r] = dot<T>(q[r], x.k[i]);
                 group_sums(s, l.G);
                 float low = 0.0f, e2[U * R];
-                sc.template products<U * R, 1>(s, e2);
+                sc.template products<T, U * R, 1>(s, e2);
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
 #pragma unroll
@@ -693,7 +697,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
                 }
                 group_sums(s, l.G);
                 float e2[U];
-                sc.template products<U, 2>(s, e2);
+                sc.template products<T, U, 2>(s, e2);
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
                     float dp = s[2 * i + 1];
@@ -799,7 +803,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
         const int64_t beg = clip(pt_off[p0 + i0]);
         int64_t total = clip(pt_off[p0 + i0 + n0]) - beg;
         if (total < 0) total = 0;
-        float gk[W] = {}, gv[W] = {};
+        float gk[W] = {}, gv[W] = {}, gs = 0.0f;  // gs: the slope's, of a lane's one head
         Raw x, y;
         float p3[3] = {};
         int32_t starts = 0, cur = -1;  // FLAT: where the lane's point's list starts; the point the sums are of
@@ -912,7 +916,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                 }
                 group_sums(s, l.G);
                 float e2[U];
-                sc.template products<U, 2>(s, e2);
+                sc.template products<T, U, 2>(s, e2);
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
                     const int h = at.head * Rq + rr[i];
@@ -949,12 +953,16 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                                 lds_add(&tab[__umul24(b.nb + (pu[i] >> 8 & 255u), (uint32_t)a.H) + h], ds);
                                 lds_add(&tab[__umul24(2 * b.nb + (pu[i] >> 16), (uint32_t)a.H) + h], ds);
                             }
-                            if (b.slope) lds_add(&tab[3 * b.nb * a.H + h], ds * pd[i]);
+                            if (Rq == 1) gs = fmaf(ds, pd[i], gs);
+                            else if (b.slope) lds_add(&tab[3 * b.nb * a.H + h], ds * pd[i]);
                         }
                     }
                 }
             }
             __builtin_amdgcn_wave_barrier();
+        }
+        if constexpr (TAB) {
+            if (Rq == 1 && b.slope && at.chan == 0 && at.on) lds_add(&tab[3 * b.nb * a.H + at.head], gs);
         }
         if (!FLAT) {
 #pragma unroll
