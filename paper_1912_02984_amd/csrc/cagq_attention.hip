@@ -28,11 +28,11 @@
 // Measured on indoor scenes (4 x 81920 points, 8192 centers of 32, 8 heads of
 // 32 channels in bfloat16: 779000 pairs, of which each reads two rows of 512
 // bytes): forward 100 us, gradients 112 us at the centers and 250 us at the
-// points. The caches' misses bound all three: 0.57, 0.59 and 1.35 GB at 5.2 to
-// 5.7 TB/s (rows are as much as a cloud's 84 MB apart in time of use, an L2
+// points. The caches' misses bound all three: 0.58, 0.60 and 1.29 GB at 5.1 to
+// 5.8 TB/s (rows are as much as a cloud's 84 MB apart in time of use, an L2
 // holds 4 MB), against 0.35 GB that the forward cannot do without; its loads
 // without any arithmetic take 97 us. Short rows are bound by issue instead:
-// whole contexts (2 x 3001 centers, 1.28 M pairs, 6 heads of 16) 86 us, of
+// whole contexts (2 x 3001 centers, 1.28 M pairs, 6 heads of 16) 90 us, of
 // which 45 are vector instructions, the rest of it the longest lists' ends and
 // the L1's 64 lanes' gathers. A few short lists take a chain of cold loads: 8 us.
 #include <initializer_list>
