@@ -437,7 +437,8 @@ typedef struct cagq_bias {
  * point) to the next, heads and channels of a row being contiguous; 0 means
  * densely packed rows. They let q, k and v be parts of one projection.
  * scale multiplies q.k. cap > 0 caps the scaled products: cap * tanh(x / cap);
- * cap = 0 leaves them (2 * cap and 3 * scale / cap must be finite). 1 <= D <= CAGQ_MAX_HEAD_DIM, 1 <= H <= CAGQ_MAX_HEADS.
+ * cap = 0 leaves them (2 * cap and 3 * scale / cap must be finite).
+ * 1 <= D <= CAGQ_MAX_HEAD_DIM, 1 <= H <= CAGQ_MAX_HEADS.
  */
 typedef struct cagq_attn {
     int32_t dtype, H, Hkv, D;

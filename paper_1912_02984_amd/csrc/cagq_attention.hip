@@ -1144,7 +1144,7 @@ bool flat_of(int64_t points, int64_t slots, const Attn& a, const Lanes& l) {
 
 // The launch of the gradient at the points. Points are walked in a row by a
 // slot where the places fit 32 bits; several of them where there are enough
-// for more than two rounds of the card's waves (3072 of them).
+// for more than two rounds of the card's waves.
 struct BackShape {
     bool flat;
     Walk walk;

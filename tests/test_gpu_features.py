@@ -188,7 +188,8 @@ def test_attention_of_tangled_groups(dt, H, Hkv, D, M):
     (F32, 2, 1, 64, 66000, 400, 3), (F16, 4, 2, 128, 66000, 400, 3),  # several points a slot, shared heads
     (BF16, 2, 1, 8, 200, 1100, 140), (F32, 1, 1, 3, 200, 1100, 140),  # a workgroup to a list, not cut
     (F16, 1, 1, 3, 500, 3, 2000), (BF16, 4, 4, 32, 40, 900, 2),      # cut, rows off 16 bytes; a list per slot
-    (F16, 3, 3, 32, 700, 500, 8), (F32, 3, 3, 32, 700, 500, 9)])     # either side of that
+    (F16, 3, 3, 32, 700, 500, 8), (F32, 3, 3, 32, 700, 500, 9),      # either side of that
+    (F32, 2, 1, 256, 6, 300, 40), (BF16, 4, 2, 256, 6, 300, 40)])    # a row to a wave, long lists at the points
 @pytest.mark.parametrize("ragged", [False, True])
 def test_attention_ways_to_share_waves(dt, H, Hkv, D, N, M, lens, ragged):
     """Every way in which lists share waves, with fixed and ragged groups, with and without a bias."""
