@@ -101,10 +101,12 @@ struct LaneAt {
     }
 };
 
-// The rows of one cloud. BUF: a buffer of less than 2^31 bytes, rows aligned
-// to 16 bytes; an offset of kNone is past its end whatever is added to it.
-// Otherwise pointers, element by element.
+// The rows of one cloud. BUF: a buffer of at most kMostBytes, rows aligned to
+// 16 bytes. An entry that is not there (kNone) and a lane without channels
+// (kMostBytes) each bring an offset past its end, and so do both together:
+// their sum stays below 2^32. Otherwise pointers, element by element.
 constexpr uint32_t kNone = 0x80000000u;
+constexpr uint32_t kMostBytes = kNone - 4096;
 
 template <typename T, bool BUF>
 struct Rows {
@@ -118,7 +120,7 @@ struct Rows {
     __device__ __forceinline__ Rows(const T* first, int64_t row_, uint32_t bytes, int lane_elem, int n_) {
         if constexpr (BUF) {
             rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, (int)bytes, 0x00027000);
-            lane_off = n_ > 0 ? (uint32_t)lane_elem * (uint32_t)sizeof(T) : kNone;
+            lane_off = n_ > 0 ? (uint32_t)lane_elem * (uint32_t)sizeof(T) : kMostBytes;
         } else {
             base = first + lane_elem;
             row = row_;
@@ -1046,7 +1048,7 @@ bool vectors(const Groups& g, const Attn& a, std::initializer_list<const void*> 
     for (const void* p : ptrs)
         if ((uintptr_t)p & 15) return false;
     // a cloud's rows in one buffer
-    const int64_t most = (int64_t)(kNone - 4096) / (int64_t)sizeof(T);
+    const int64_t most = (int64_t)kMostBytes / (int64_t)sizeof(T);
     const int64_t qd = (int64_t)a.H * a.D;
     return a.k_row <= most / g.N && a.v_row <= most / g.N && a.q_row <= most / g.M && qd <= most / g.M;
 }
