@@ -710,6 +710,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
                             k[i] = Raw{0, 0, 0, 0};
                             x = kNegInf;
                             dp = 0.0f;
+                            e2[i] = 0.5f;
                         }
                     }
                     const float p = there[i] ? weight(x - z) : 0.0f;
@@ -930,6 +931,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                             q[i] = go[i] = Raw{0, 0, 0, 0};
                             v = kNegInf;
                             dp = 0.0f;
+                            e2[i] = 0.5f;
                         }
                     }
                     const float p = there[i] ? weight(v - st[i].x) : 0.0f;

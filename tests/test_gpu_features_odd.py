@@ -34,6 +34,36 @@ def _odd(t, where):
     return t
 
 
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("cap", [0.0, 9.0, 100.0])
+@pytest.mark.parametrize("way", range(len(WAYS)))
+def test_pairs_masked_by_the_bias(dt, cap, way):
+    """A pair whose bias is -infinity contributes nothing, whatever k and v hold: not to the outputs, nor to any
+    gradient. Points far away on one axis are masked for all heads, on another for the first head alone."""
+    rng = np.random.default_rng(101 + way)
+    c = _groups(rng, **WAYS[way])
+    c.points[:, ::3, 0] -= 100.0
+    c.points[:, 1::4, 1] -= 100.0
+    for H, Hkv, D in ((4, 4, 16), (8, 2, 16), (3, 3, 24)):
+        q, k, v, dout = (_features(rng, (2, n, h, D), dt) for n, h in ((c.M, H), (c.N, Hkv), (c.N, Hkv), (c.M, H)))
+        table, edges, _ = F.rand_bias(rng, H, 6, False)
+        edges[:2, 0] = -50.0
+        table[0, 0] = -np.inf
+        table[1, 0, 0] = -np.inf
+        bias = (table, edges, None)
+        u, _ = c.places(edges)
+        dead = np.isinf(table[0][u[:, 0]] + table[1][u[:, 1]])  # [pairs][H]
+        live = np.zeros((2 * c.N, Hkv), bool)
+        np.logical_or.at(live, c.pt, ~dead.reshape(-1, Hkv, H // Hkv).all(2))
+        held = np.zeros(2 * c.N, bool)
+        held[c.pt] = True
+        assert (held[:, None] & ~live).any() and live.any()
+        zero = torch.from_numpy(~live).reshape(2, c.N, Hkv)
+        k, v = (torch.where(zero[..., None], torch.zeros((), dtype=dt), t) for t in (k, v))
+        want = F.attention(c, q, k, v, bias, None, cap, dout)
+        F.check(_attend(c, q, _odd(k, zero), _odd(v, zero), bias, None, cap, dout), want, f"{dt} {cap} {way} {H}")
+
+
 @pytest.mark.parametrize("dt,D", [(BF16, 24), (F16, 48), (F32, 12), (F32, 20), (BF16, 40), (BF16, 16)])
 @pytest.mark.parametrize("cap", [0.0, 9.0, 100.0])
 @pytest.mark.parametrize("way", range(len(WAYS)))
