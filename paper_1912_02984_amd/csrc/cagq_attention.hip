@@ -713,8 +713,9 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
                             e2[i] = 0.5f;
                         }
                     }
+                    // an entry that is not there: its zeros times a q or dout that is not finite are none
                     const float p = there[i] ? weight(x - z) : 0.0f;
-                    const float pdp = p * dp, sl = Score::slack(e2[i]);
+                    const float pdp = there[i] ? p * dp : 0.0f, sl = there[i] ? Score::slack(e2[i]) : 0.0f;
                     sum += pdp;
                     ones += p;
                     add_channels<T>(acc, pdp * sl, k[i]);

@@ -81,3 +81,53 @@ def test_a_point_in_no_group(dt, D, cap, way):
         for x in (NAN, INF):
             k[:, 0], v[:, 0] = x, x
             F.check(_attend(c, q, k, v, bias, None, cap, dout), want, f"{dt} {D} {cap} {way} {H} {x}")
+
+
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("cap", [0.0, 9.0, 100.0])
+@pytest.mark.parametrize("way", range(len(WAYS)))
+def test_groups_of_nothing(dt, cap, way):
+    """Padded centers: groups without a slot, and with masked slots alone. What their q and dout hold reaches
+    nothing; their own rows of out and dq are zeros."""
+    rng = np.random.default_rng(151 + way)
+    c = _groups(rng, **WAYS[way])
+    H, Hkv, D = 4, 2, 24
+    some = np.zeros(2 * c.M, bool)
+    some[c.row] = True
+    none = rng.random(2 * c.M) < 0.3
+    none[:2] = True
+    idx = c.idx.reshape(2 * c.M, -1) if c.off is None else c.idx
+    if c.off is None:
+        idx[none] = -1
+    else:
+        idx[np.isin(np.repeat(np.arange(2 * c.M), np.diff(c.off)), np.flatnonzero(none))] = c.N
+    c = F.Case(2, c.N, c.M, c.idx, n_valid=c.n_valid, off=c.off, rng=rng)
+    none |= ~some
+    q, k, v, dout = (_features(rng, (2, n, h, D), dt) for n, h in ((c.M, H), (c.N, Hkv), (c.N, Hkv), (c.M, H)))
+    bias = F.rand_bias(rng, H, 5, True)
+    want = F.attention(c, q, k, v, bias, None, cap, dout)
+    rows = torch.from_numpy(none).reshape(2, c.M, 1).expand(2, c.M, H)
+    got = _attend(c, _odd(q, rows), k, v, bias, None, cap, _odd(dout, rows))
+    F.check(got, want, f"{dt} {cap} {way}")
+    assert (got["dq"].cpu()[rows] == 0).all() and (got["out"].cpu()[rows] == 0).all()
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_a_score_at_its_cap(dt):
+    """An infinite q under a cap: every score is the cap or its negative, the weights are finite, and the
+    tanh is flat there, so that nothing comes back to q. Lists that end inside a round. (At most 9 entries, a score's
+    weight off by less than 30 steps of 2^-24, values below 5, a point in at most 40 lists.)"""
+    rng = np.random.default_rng(171)
+    c = _groups(rng, 60, 50, lens=[1, 2, 5, 9], masked=0.0)
+    q, k, v, dout = (_features(rng, (2, n, 2, 16), dt) for n in (50, 60, 60, 50))
+    k = k.abs() + 0.5
+    none = (None, None, None)
+    big = torch.where(torch.arange(16) == 3, 1e30, 0.0).to(dt).expand(q.shape).contiguous()
+    want = F.attention(c, big, k, v, none, None, 3.0, dout)
+    got = _attend(c, torch.where(big > 0, INF, 0.0).to(dt), k, v, none, None, 3.0, dout)
+    zero = lambda t: torch.zeros_like(t, dtype=torch.float64)  # noqa: E731
+    u = torch.full((), 2.0 ** -16, dtype=torch.float64)
+    F.check({n: got[n] for n in ("out", "dv", "dq")}, {
+        "out": (want["out"][0], F.half_step(dt) * want["out"][0].abs() + u),
+        "dv": (want["dv"][0], F.half_step(dt) * want["dv"][0].abs() + 64 * u),
+        "dq": (zero(q), u)}, str(dt))
