@@ -743,7 +743,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
 }
 
 // Gradient at the points, over the centers that hold each; and the bias's
-// gradient, which a wave sums in a table of its own in LDS.
+// gradient, which a wave sums in a table of its own in LDS, of its pass's heads.
 // FLAT: a slot takes P points in a row and walks through their lists as one
 // (lists here are a few entries long: a list per slot would leave most of a
 // round's rows empty, and the wave would wait for the longest). A round's rows
@@ -769,7 +769,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
     const int rows_n = Rounds<FLAT, U>::rows_n(l), hp = l.Hc * Rq, hw = (int)blockIdx.y * hp;
     const int hn = a.H - hw < hp ? a.H - hw : hp;
     Chunk ck(s_lds + Score::floats(b), rows_n, sc, hp);
-    const int entries = (3 * b.nb + 1) * a.H;
+    const int rows_t = 3 * b.nb + 1, entries = rows_t * hp;  // of a wave's table: this pass's heads
     float* s_tab = s_lds + Score::floats(b) + waves_b * Chunk::floats(sc.placed(), rows_n, hp);
     float* tab = s_tab + wave * entries;
     if constexpr (TAB) {
@@ -923,7 +923,6 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                 sc.template products<T, U, 2>(s, e2);
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
-                    const int h = at.head * Rq + rr[i];
                     float dp = s[2 * i + 1];
                     float v = s[2 * i] + bi[i];
                     if (__any(bi[i] == kNegInf)) {
@@ -953,13 +952,14 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                     add_channels<T>(gv, p, go[i]);
                     if constexpr (TAB) {
                         if (at.chan == 0 && there[i] && at.on) {
+                            const int h = at.head * Rq + rr[i] - hw;
                             if (b.nb > 0) {
-                                lds_add(&tab[__umul24(pu[i] & 255u, (uint32_t)a.H) + h], ds);
-                                lds_add(&tab[__umul24(b.nb + (pu[i] >> 8 & 255u), (uint32_t)a.H) + h], ds);
-                                lds_add(&tab[__umul24(2 * b.nb + (pu[i] >> 16), (uint32_t)a.H) + h], ds);
+                                lds_add(&tab[__umul24(pu[i] & 255u, (uint32_t)hp) + h], ds);
+                                lds_add(&tab[__umul24(b.nb + (pu[i] >> 8 & 255u), (uint32_t)hp) + h], ds);
+                                lds_add(&tab[__umul24(2 * b.nb + (pu[i] >> 16), (uint32_t)hp) + h], ds);
                             }
                             if (Rq == 1) gs = fmaf(ds, pd[i], gs);
-                            else if (b.slope) lds_add(&tab[3 * b.nb * a.H + h], ds * pd[i]);
+                            else if (b.slope) lds_add(&tab[3 * b.nb * hp + h], ds * pd[i]);
                         }
                     }
                 }
@@ -967,7 +967,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
             __builtin_amdgcn_wave_barrier();
         }
         if constexpr (TAB) {
-            if (Rq == 1 && b.slope && at.chan == 0 && at.on) lds_add(&tab[3 * b.nb * a.H + at.head], gs);
+            if (Rq == 1 && b.slope && at.chan == 0 && at.on) lds_add(&tab[3 * b.nb * hp + at.head - hw], gs);
         }
         if (!FLAT) {
 #pragma unroll
@@ -982,11 +982,11 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
     });
     if constexpr (TAB) {
         __syncthreads();
-        const int64_t blk = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-        for (int e = threadIdx.x; e < entries; e += blockDim.x) {
+        for (int e = threadIdx.x; e < rows_t * hn; e += blockDim.x) {
+            const int r = e / hn, h = e - r * hn;
             float x = 0.0f;
-            for (int w = 0; w < waves_b; ++w) x += s_tab[w * entries + e];
-            part[blk * entries + e] = x;
+            for (int w = 0; w < waves_b; ++w) x += s_tab[w * entries + r * hp + h];
+            part[((int64_t)blockIdx.x * rows_t + r) * a.H + hw + h] = x;
         }
     }
 }
@@ -1166,7 +1166,7 @@ BackShape back_shape(const Groups& g, int32_t B, const Attn& a, const Bias& b, c
     r.walk = r.flat ? make_walk(B, g.N, l.S, (int32_t)(P < 1 ? 1 : P > most ? most : P)) : make_walk(B, g.N, 1, 1);
     const int rows = r.flat ? Rounds<true, kBackUnroll>::rows_n(l) : Rounds<false, kBackUnroll>::rows_n(l);
     size_t floats = Chunk::floats(placed(b), rows, l.Hc * (a.H / a.Hkv));
-    if (tab) floats += (size_t)(3 * b.nb + 1) * a.H;
+    if (tab) floats += (size_t)(3 * b.nb + 1) * l.Hc * (a.H / a.Hkv);
     r.sh = shape_of(b, floats);
     r.blocks = blocks_of(r.walk.units, r.sh.waves, r.flat || tab ? kAtBlocks : kAtMany);
     return r;
@@ -1207,7 +1207,7 @@ hipError_t backward(const Groups& g, int32_t B, const Attn& a, const Bias& b, co
     const std::false_type no;
     e = buf ? (tab ? with(yes, yes) : with(yes, no)) : (tab ? with(no, yes) : with(no, no));
     if (e != hipSuccess || !tab) return e;
-    return launch_bias_reduce(part, (int32_t)r.blocks * lp.passes, b, dtable, dslope, s);
+    return launch_bias_reduce(part, (int32_t)r.blocks, b, dtable, dslope, s);
 }
 
 Lanes lanes_of(int32_t dtype, int32_t heads, int32_t D) {
@@ -1225,7 +1225,7 @@ size_t group_attention_bytes(const Groups& g, int32_t B, const Attn& a, int32_t 
     if (!placed(b)) return stat;
     const Lanes l = lanes_of(dtype, a.Hkv, a.D);
     const BackShape r = back_shape(g, B, a, b, l, true);
-    return stat + (size_t)r.blocks * l.passes * (3 * b.nb + 1) * b.H * 4;
+    return stat + (size_t)r.blocks * (3 * b.nb + 1) * b.H * 4;
 }
 
 hipError_t launch_group_attention(const Groups& g, int32_t B, const Attn& a, int32_t dtype, const Bias& b, void* out,
