@@ -36,7 +36,6 @@
 // which 45 are vector instructions, the rest of it the longest lists' ends and
 // the L1's 64 lanes' gathers. A few short lists take a chain of cold loads: 8 us.
 #include <initializer_list>
-#include <type_traits>
 
 #include "cagq_features.h"
 
@@ -53,6 +52,7 @@ constexpr int kAtWaves = kAtThreads / kWave;
 constexpr int kAtBlocks = 256 * 3;
 constexpr int kAtMany = 1 << 16;
 constexpr int kAtLds = 144 << 10;    // LDS of a workgroup: edges, table, chunks, and the waves' gradient tables
+constexpr int kCuLds = 160 << 10;    // what a workgroup can have at most
 constexpr int kPoints = 16;          // most points in a row whose lists one slot walks (FLAT)
 constexpr int kJoinFloats = 2048;    // H * D up to which a workgroup's waves join their parts in LDS
 // Caps above it: see Score::products. Of 2-byte features a score is off by some
@@ -1149,63 +1149,63 @@ bool flat_of(int64_t points, int64_t slots, const Attn& a, const Lanes& l) {
 
 // The launch of the gradient at the points. Points are walked in a row by a
 // slot where the places fit 32 bits; several of them where there are enough
-// for more than two rounds of the card's waves.
+// for more than two rounds of the card's waves. Fewer slots where one wave's
+// chunk and table of the bias's gradient take more LDS than a CU has (128 heads
+// of at most 16 bytes that share one key's, 64 buckets: 168 KB with 64 slots).
 struct BackShape {
     bool flat;
+    Lanes l;
     Walk walk;
     Shape sh;
     uint32_t blocks;
 };
 
-BackShape back_shape(const Groups& g, int32_t B, const Attn& a, const Bias& b, const Lanes& l, bool tab) {
+BackShape back_shape(const Groups& g, int32_t B, const Attn& a, const Bias& b, Lanes l, bool tab) {
     BackShape r;
     const int64_t points = (int64_t)B * g.N;
     r.flat = g.idx_len < (1ll << 31) && flat_of(points, g.idx_len, a, l);
+    for (;; l.S >>= 1) {
+        const int rows = r.flat ? Rounds<true, kBackUnroll>::rows_n(l) : Rounds<false, kBackUnroll>::rows_n(l);
+        size_t floats = Chunk::floats(placed(b), rows, l.Hc * (a.H / a.Hkv));
+        if (tab) floats += (size_t)(3 * b.nb + 1) * l.Hc * (a.H / a.Hkv);
+        r.sh = shape_of(b, floats);
+        if (r.sh.lds <= kCuLds || l.S == 1) break;
+    }
+    r.l = l;
     const int32_t step = l.Hc * l.G, most = step < kPoints ? step : kPoints;
     const int64_t P = points / ((int64_t)l.S * 8192);
     r.walk = r.flat ? make_walk(B, g.N, l.S, (int32_t)(P < 1 ? 1 : P > most ? most : P)) : make_walk(B, g.N, 1, 1);
-    const int rows = r.flat ? Rounds<true, kBackUnroll>::rows_n(l) : Rounds<false, kBackUnroll>::rows_n(l);
-    size_t floats = Chunk::floats(placed(b), rows, l.Hc * (a.H / a.Hkv));
-    if (tab) floats += (size_t)(3 * b.nb + 1) * l.Hc * (a.H / a.Hkv);
-    r.sh = shape_of(b, floats);
     r.blocks = blocks_of(r.walk.units, r.sh.waves, r.flat || tab ? kAtBlocks : kAtMany);
     return r;
 }
 
-template <typename T, bool BUF, bool FLAT, bool TAB>
-hipError_t back_points(const Groups& g, const Attn& a, const Bias& b, const Lanes& l, const BackShape& r,
-                       const int64_t* pt_off, const int32_t* pt_center, int64_t capacity, const float2* stat,
-                       const void* dout, void* dk, void* dv, float* part, hipStream_t s) {
-    auto kern = k_at_back_p<T, BUF, FLAT, TAB>;
-    hipError_t e = allow_lds(kern, r.sh.lds);
-    if (e != hipSuccess) return e;
-    kern<<<dim3(r.blocks, l.passes), r.sh.waves * kWave, r.sh.lds, s>>>(
-        g, b, a, l, r.walk, pt_off, pt_center, capacity, stat, (const T*)dout, (T*)dk, (T*)dv, part);
-    return hipGetLastError();
+template <typename T, bool BUF>
+auto points_kernel(bool flat, bool tab) {
+    return flat ? (tab ? k_at_back_p<T, BUF, true, true> : k_at_back_p<T, BUF, true, false>)
+                : (tab ? k_at_back_p<T, BUF, false, true> : k_at_back_p<T, BUF, false, false>);
 }
 
 template <typename T>
 hipError_t backward(const Groups& g, int32_t B, const Attn& a, const Bias& b, const int64_t* pt_off,
                     const int32_t* pt_center, int64_t capacity, const float* lse, const void* dout, void* dq, void* dk,
                     void* dv, float* dtable, float* dslope, void* ws, hipStream_t s) {
-    const Lanes lc = make_lanes<T>(a.H, a.D), lp = make_lanes<T>(a.Hkv, a.D);
+    const Lanes lc = make_lanes<T>(a.H, a.D);
     float2* stat = (float2*)ws;
     float* part = (float*)((char*)ws + align256((size_t)g.rows * a.H * 8));
     const bool buf = vectors<T>(g, a, {a.q, a.k, a.v, dout, dq, dk, dv});
     const bool ec = each_of(g.rows, g.idx_len, lc), tab = dtable || dslope;
-    auto fc = buf ? (ec ? back_centers<T, true, true> : back_centers<T, true, false>)
-                  : (ec ? back_centers<T, false, true> : back_centers<T, false, false>);
-    hipError_t e = fc(g, B, a, b, lc, lse, dout, dq, stat, s);
+    // what can fail, before anything is enqueued
+    const BackShape r = back_shape(g, B, a, b, make_lanes<T>(a.Hkv, a.D), tab);
+    auto points = buf ? points_kernel<T, true>(r.flat, tab) : points_kernel<T, false>(r.flat, tab);
+    hipError_t e = allow_lds(points, r.sh.lds);
     if (e != hipSuccess) return e;
-    const BackShape r = back_shape(g, B, a, b, lp, tab);
-    auto with = [&](auto bufc, auto tabc) {
-        constexpr bool BUF = decltype(bufc)::value, TAB = decltype(tabc)::value;
-        return (r.flat ? back_points<T, BUF, true, TAB> : back_points<T, BUF, false, TAB>)(
-            g, a, b, lp, r, pt_off, pt_center, capacity, stat, dout, dk, dv, part, s);
-    };
-    const std::true_type yes;
-    const std::false_type no;
-    e = buf ? (tab ? with(yes, yes) : with(yes, no)) : (tab ? with(no, yes) : with(no, no));
+    auto centers = buf ? (ec ? back_centers<T, true, true> : back_centers<T, true, false>)
+                       : (ec ? back_centers<T, false, true> : back_centers<T, false, false>);
+    e = centers(g, B, a, b, lc, lse, dout, dq, stat, s);
+    if (e != hipSuccess) return e;
+    points<<<dim3(r.blocks, r.l.passes), r.sh.waves * kWave, r.sh.lds, s>>>(
+        g, b, a, r.l, r.walk, pt_off, pt_center, capacity, stat, (const T*)dout, (T*)dk, (T*)dv, part);
+    e = hipGetLastError();
     if (e != hipSuccess || !tab) return e;
     return launch_bias_reduce(part, (int32_t)r.blocks, b, dtable, dslope, s);
 }

@@ -131,3 +131,16 @@ def test_a_score_at_its_cap(dt):
         "out": (want["out"][0], F.half_step(dt) * want["out"][0].abs() + u),
         "dv": (want["dv"][0], F.half_step(dt) * want["dv"][0].abs() + 64 * u),
         "dq": (zero(q), u)}, str(dt))
+
+
+@pytest.mark.parametrize("dt,H,Hkv,D", [(BF16, 128, 1, 8), (F16, 124, 1, 3), (F32, 128, 1, 4), (F32, 126, 1, 1),
+                                        (BF16, 128, 2, 8), (F16, 128, 128, 8)])
+@pytest.mark.parametrize("N,M,K", [(60, 9, 12), (3, 40, 30)])
+def test_most_heads_and_buckets(dt, H, Hkv, D, N, M, K):
+    """The gradient's table at its largest, where points are walked in a row and where a wave takes a point's list."""
+    rng = np.random.default_rng(H + D + N)
+    c = F.rand_groups(rng, 2, N, M, K, masked=0.1)
+    q, k, v, dout = (_features(rng, (2, n, h, D), dt) for n, h in ((M, H), (N, Hkv), (N, Hkv), (M, H)))
+    bias = F.rand_bias(rng, H, 64, True)
+    want = F.attention(c, q, k, v, bias, None, 0.0, dout)
+    F.check(_attend(c, q, k, v, bias, None, 0.0, dout), want, f"{dt} {H} {D} {N}")
