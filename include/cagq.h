@@ -495,7 +495,10 @@ CAGQ_API int cagq_point_lists(const cagq_groups* g, int64_t* pt_off, int32_t* pt
  * [B][M][H][D], dense) of its output; lse as the forward call wrote it,
  * pt_off and pt_center as cagq_point_lists wrote them for the same groups
  * (`capacity` entries). With dp_i = dout.v_i, p_i = exp(s_i - lse) and
- * ds_i = p_i * (dp_i - sum_i p_i dp_i):
+ * ds_i = p_i * (dp_i - sum_i p_i dp_i)
+ * (where |lse| > 256, p_i is divided by the group's sum of them: beside a large
+ * lse, such as that of a group whose slots all have a bias of the type's lowest
+ * value, fp32 has no room for the log of the weights' sum):
  *   dq  device [B][M][H][D], dk and dv device [B][N][Hkv][D], dense, of the
  *       features' type, written whole (points in no group get zeros);
  *   dtable device float [3][buckets][H], dslope device float [H]: the sums of

@@ -59,6 +59,12 @@ constexpr int kJoinFloats = 2048;    // H * D up to which a workgroup's waves jo
 // 2^-9 of its products' sizes anyway.
 template <typename T>
 constexpr float kWideCap = sizeof(T) == 4 ? 0.0f : 64.0f;
+// Groups whose |lse| is above it: beside such an lse the log of the weights'
+// sum is (partly) rounded away - all of it where a whole group has scores of the
+// type's lowest value - and weights exp(s - lse) sum up to as much as their
+// number instead of 1. The gradients divide them by their sum. Below, a weight
+// is off by less than 2^-16 by it.
+constexpr float kFarLse = 256.0f;
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
@@ -619,11 +625,13 @@ __global__ __launch_bounds__(kAtThreads) void k_at_join(Partial part, int64_t ro
 // the list, in fp32. The weights' sum is 1 but for the rounding of lse, which
 // all of a list share; dividing delta by it keeps the sum of a list's ds at 0,
 // on which the sums over many lists in the bias's gradient rely.
-// stat: (lse, delta) of each row and head, for the points.
+// stat: (lse, delta) of each row and head, for the points; share: what their
+// weights are multiplied by, of groups above kFarLse alone.
 template <typename T, bool BUF, bool EACH>
 __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn a, Lanes l, Walk walk,
                                                           const float* __restrict__ lse, const T* __restrict__ dout,
-                                                          T* __restrict__ dq, float2* __restrict__ stat) {
+                                                          T* __restrict__ dq, float2* __restrict__ stat,
+                                                          float* __restrict__ share) {
     constexpr int W = kVec<T>;
     constexpr int U = kUnroll<1>;
     extern __shared__ __align__(16) float s_lds[];
@@ -735,10 +743,15 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
         }
         if (!(EACH ? at.on && live_row : at.on && at.slot == 0)) return;
         const float delta = ones > 0.0f ? sum / ones : sum;
+        const bool far = fabsf(z) > kFarLse;
+        const float part = far && ones > 0.0f ? 1.0f / ones : 1.0f;
 #pragma unroll
-        for (int w = 0; w < W; ++w) acc[w] = a.scale * fmaf(-delta, acd[w], acc[w]);
+        for (int w = 0; w < W; ++w) acc[w] = a.scale * part * fmaf(-delta, acd[w], acc[w]);
         store_channels<T, BUF>(dq + rh * a.D + at.chan, at.n, acc);
-        if (at.chan == 0) stat[rh] = make_float2(z, delta);
+        if (at.chan == 0) {
+            stat[rh] = make_float2(z, delta);
+            if (far) share[rh] = part;
+        }
     });
 }
 
@@ -755,7 +768,8 @@ template <typename T, bool BUF, bool FLAT, bool TAB>
 __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn a, Lanes l, Walk walk,
                                                           const int64_t* __restrict__ pt_off,
                                                           const int32_t* __restrict__ pt_center, int64_t capacity,
-                                                          const float2* __restrict__ stat, const T* __restrict__ dout,
+                                                          const float2* __restrict__ stat,
+                                                          const float* __restrict__ share, const T* __restrict__ dout,
                                                           T* __restrict__ dk, T* __restrict__ dv,
                                                           float* __restrict__ part) {
     constexpr int W = kVec<T>;
@@ -803,6 +817,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
         const RowsOut<T, BUF> dkr(dk + p0 * kd, kd, at.head * a.D + at.chan, at.n);
         const RowsOut<T, BUF> dvr(dv + p0 * kd, kd, at.head * a.D + at.chan, at.n);
         const float2* st0 = stat + c0 * a.H;
+        const float* share0 = share + c0 * a.H;
         auto clip = [&](int64_t x) { return x < 0 ? 0 : x > capacity ? capacity : x; };
         const int64_t beg = clip(pt_off[p0 + i0]);
         int64_t total = clip(pt_off[p0 + i0 + n0]) - beg;
@@ -924,9 +939,14 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
                     float dp = s[2 * i + 1];
-                    float v = s[2 * i] + bi[i];
-                    if (__any(bi[i] == kNegInf)) {
+                    float v = s[2 * i] + bi[i], part = 1.0f;
+                    if (__any(bi[i] == kNegInf || fabsf(st[i].x) > kFarLse)) {
                         rare();
+                        if (there[i] && fabsf(st[i].x) > kFarLse) {
+                            const float* r0 = ck.row(at_row[i]);
+                            const int64_t c = BUF ? (int64_t)ck.field(r0, kStat) : (int64_t)ck.field(r0, kKey) * a.H;
+                            part = share0[c + at.head * Rq + rr[i]];
+                        }
                         if (bi[i] == kNegInf) {
                             q[i] = go[i] = Raw{0, 0, 0, 0};
                             v = kNegInf;
@@ -934,7 +954,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                             e2[i] = 0.5f;
                         }
                     }
-                    const float p = there[i] ? weight(v - st[i].x) : 0.0f;
+                    const float p = there[i] ? weight(v - st[i].x) * part : 0.0f;
                     const float ds = there[i] ? p * (dp - st[i].y) : 0.0f;
                     const float da = there[i] ? ds * Score::slack(e2[i]) : 0.0f;
                     if (FLAT) {
@@ -993,7 +1013,8 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
 
 // ------------------------------------------------------------------ host side
 
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+// What the centers' pass of the gradients leaves for the points': (lse, delta) and a share for each row and head.
+size_t stat_bytes(int64_t rh) { return ((size_t)rh * 12 + 255) & ~(size_t)255; }
 
 // Whether every slot of a wave takes a list of its own: lists short, and the
 // shorter the fewer of them that takes. (Mean lengths of 5 and 8, 5870 and 4542
@@ -1125,14 +1146,14 @@ hipError_t forward(const Groups& g, int32_t B, const Attn& a, const Bias& b, voi
 
 template <typename T, bool BUF, bool EACH>
 hipError_t back_centers(const Groups& g, int32_t B, const Attn& a, const Bias& b, const Lanes& l, const float* lse,
-                        const void* dout, void* dq, float2* stat, hipStream_t s) {
+                        const void* dout, void* dq, float2* stat, float* share, hipStream_t s) {
     const Walk w = make_walk(B, g.M, EACH ? l.S : 1, 1);
     const Shape sh = shape_of(b, Chunk::floats(placed(b), Rounds<EACH, kUnroll<1>>::rows_n(l), l.Hc));
     auto kern = k_at_back_c<T, BUF, EACH>;
     hipError_t e = allow_lds(kern, sh.lds);
     if (e != hipSuccess) return e;
     kern<<<dim3(blocks_of(w.units, sh.waves, EACH ? kAtBlocks : kAtMany), l.passes), sh.waves * kWave, sh.lds, s>>>(
-        g, b, a, l, w, lse, (const T*)dout, (T*)dq, stat);
+        g, b, a, l, w, lse, (const T*)dout, (T*)dq, stat, share);
     return hipGetLastError();
 }
 
@@ -1190,8 +1211,10 @@ hipError_t backward(const Groups& g, int32_t B, const Attn& a, const Bias& b, co
                     const int32_t* pt_center, int64_t capacity, const float* lse, const void* dout, void* dq, void* dk,
                     void* dv, float* dtable, float* dslope, void* ws, hipStream_t s) {
     const Lanes lc = make_lanes<T>(a.H, a.D);
+    const int64_t rh = (int64_t)g.rows * a.H;
     float2* stat = (float2*)ws;
-    float* part = (float*)((char*)ws + align256((size_t)g.rows * a.H * 8));
+    float* share = (float*)(stat + rh);
+    float* part = (float*)((char*)ws + stat_bytes(rh));
     const bool buf = vectors<T>(g, a, {a.q, a.k, a.v, dout, dq, dk, dv});
     const bool ec = each_of(g.rows, g.idx_len, lc), tab = dtable || dslope;
     // what can fail, before anything is enqueued
@@ -1201,10 +1224,10 @@ hipError_t backward(const Groups& g, int32_t B, const Attn& a, const Bias& b, co
     if (e != hipSuccess) return e;
     auto centers = buf ? (ec ? back_centers<T, true, true> : back_centers<T, true, false>)
                        : (ec ? back_centers<T, false, true> : back_centers<T, false, false>);
-    e = centers(g, B, a, b, lc, lse, dout, dq, stat, s);
+    e = centers(g, B, a, b, lc, lse, dout, dq, stat, share, s);
     if (e != hipSuccess) return e;
     points<<<dim3(r.blocks, r.l.passes), r.sh.waves * kWave, r.sh.lds, s>>>(
-        g, b, a, r.l, r.walk, pt_off, pt_center, capacity, stat, (const T*)dout, (T*)dk, (T*)dv, part);
+        g, b, a, r.l, r.walk, pt_off, pt_center, capacity, stat, share, (const T*)dout, (T*)dk, (T*)dv, part);
     e = hipGetLastError();
     if (e != hipSuccess || !tab) return e;
     return launch_bias_reduce(part, (int32_t)r.blocks, b, dtable, dslope, s);
@@ -1221,7 +1244,7 @@ size_t group_attention_bytes(const Groups& g, int32_t B, const Attn& a, int32_t 
         const Split sp = split_of(g, a.H * a.D);
         return sp.parts > 1 ? (size_t)sp.parts * g.rows * a.H * (2 + a.D) * 4 : 0;
     }
-    const size_t stat = align256((size_t)g.rows * a.H * 8);
+    const size_t stat = stat_bytes((int64_t)g.rows * a.H);
     if (!placed(b)) return stat;
     const Lanes l = lanes_of(dtype, a.Hkv, a.D);
     const BackShape r = back_shape(g, B, a, b, l, true);

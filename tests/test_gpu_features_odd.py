@@ -144,3 +144,30 @@ def test_most_heads_and_buckets(dt, H, Hkv, D, N, M, K):
     bias = F.rand_bias(rng, H, 64, True)
     want = F.attention(c, q, k, v, bias, None, 0.0, dout)
     F.check(_attend(c, q, k, v, bias, None, 0.0, dout), want, f"{dt} {H} {D} {N}")
+
+
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("cap", [0.0, 9.0])
+@pytest.mark.parametrize("mask", [float(np.finfo(np.float32).min), -1e30, -1e9, -65504.0, 1e9])
+@pytest.mark.parametrize("way", range(len(WAYS)))
+def test_groups_all_of_one_far_score(dt, cap, mask, way):
+    """Groups whose slots all have the same score, of the type's lowest value or another far from 0: their weights
+    are alike and sum up to 1, in the gradients as well. A softmax does not change by what is added to all scores,
+    so the definition without that value is the reference (their q is 0: the scores are the value itself)."""
+    rng = np.random.default_rng(191 + way)
+    c = _groups(rng, **WAYS[way])
+    far = rng.random((2, c.M)) < 0.4
+    c.centers[far] += 100.0  # every pair of these centers in the first bucket
+    for H, Hkv, D in ((4, 4, 16), (2, 1, 20)):
+        q, k, v, dout = (_features(rng, (2, n, h, D), dt) for n, h in ((c.M, H), (c.N, Hkv), (c.N, Hkv), (c.M, H)))
+        q[torch.from_numpy(far)] = 0.0
+        table, edges, _ = F.rand_bias(rng, H, 6, False)
+        edges[:, 0] = -50.0
+        table[:, 0] = 0.0
+        want = F.attention(c, q, k, v, (table, edges, None), None, cap, dout)
+        lse, bound = want["lse"]
+        at = torch.from_numpy(far)[..., None].expand_as(lse) & torch.isfinite(lse)
+        want["lse"] = (torch.where(at, lse + mask, lse), torch.where(at, 2 * F.U * abs(mask), bound))
+        table = table.copy()
+        table[0, 0] = mask
+        F.check(_attend(c, q, k, v, (table, edges, None), None, cap, dout), want, f"{dt} {cap} {mask} {way} {H}")
