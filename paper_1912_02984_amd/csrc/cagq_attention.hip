@@ -952,6 +952,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                             v = kNegInf;
                             dp = 0.0f;
                             e2[i] = 0.5f;
+                            pd[i] = 0.0f;  // a distance that overflows, under a negative slope
                         }
                     }
                     const float p = there[i] ? weight(v - st[i].x) * part : 0.0f;

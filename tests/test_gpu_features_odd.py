@@ -171,3 +171,28 @@ def test_groups_all_of_one_far_score(dt, cap, mask, way):
         table = table.copy()
         table[0, 0] = mask
         F.check(_attend(c, q, k, v, (table, edges, None), None, cap, dout), want, f"{dt} {cap} {mask} {way} {H}")
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("way", range(len(WAYS)))
+def test_points_masked_by_their_distance(dt, way):
+    """Padded points so far away that the distance overflows: under a negative slope their bias is -infinity, and
+    they are as absent as points of masked slots, from the slope's gradient too."""
+    rng = np.random.default_rng(211 + way)
+    c = _groups(rng, **WAYS[way])
+    gone = rng.random((2, c.N)) < 0.3
+    gone[:, 1] = True
+    for H, Hkv, D, nb in ((4, 4, 16, 5), (4, 2, 16, 0)):
+        q, k, v, dout = (_features(rng, (2, n, h, D), dt) for n, h in ((c.M, H), (c.N, Hkv), (c.N, Hkv), (c.M, H)))
+        table, edges, slope = F.rand_bias(rng, H, nb, True)
+        bias = (table, edges, -np.abs(slope) - 0.1)
+        idx = c.idx.copy().reshape(-1)
+        dead = np.zeros(idx.size, bool)
+        dead[c.slot] = gone.reshape(-1)[c.pt]
+        idx[dead] = -1
+        without = F.Case(2, c.N, c.M, idx.reshape(c.idx.shape), c.n_valid, c.off, c.points, c.centers)
+        want = F.attention(without, q, k, v, bias, None, 0.0, dout)
+        points = np.where(gone[..., None], np.float32(3e30), c.points)
+        with_ = F.Case(2, c.N, c.M, c.idx, c.n_valid, c.off, points, c.centers)
+        rows = torch.from_numpy(gone)[..., None].expand(2, c.N, Hkv)
+        F.check(_attend(with_, q, _odd(k, rows), _odd(v, rows), bias, None, 0.0, dout), want, f"{dt} {way} {H}")
