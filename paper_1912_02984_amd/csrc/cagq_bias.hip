@@ -195,6 +195,7 @@ __global__ __launch_bounds__(kRbMost, 4) void k_rb_back(Groups g, Bias b, Magic 
                     }
                     atomicAdd(&s_odd[3 * b.nb * 16 + col], x * d[j]);
                     x = 0.0f;
+                    if (!(fabsf(d[j]) < __builtin_inff())) d[j] = 0.0f;  // added, and not once more below
                 }
             }
 #pragma unroll

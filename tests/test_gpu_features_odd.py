@@ -196,3 +196,36 @@ def test_points_masked_by_their_distance(dt, way):
         with_ = F.Case(2, c.N, c.M, c.idx, c.n_valid, c.off, points, c.centers)
         rows = torch.from_numpy(gone)[..., None].expand(2, c.N, Hkv)
         F.check(_attend(with_, q, _odd(k, rows), _odd(v, rows), bias, None, 0.0, dout), want, f"{dt} {way} {H}")
+
+
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_relative_bias_gradient_at_a_distance_that_overflows(dt, ragged):
+    """Gradients, finite and not, of slots at an infinite distance: each product once, as the sum has it."""
+    rng = np.random.default_rng(231)
+    H, nb = 6, 4
+    c = F.rand_groups(rng, 1, 30, 9, 0 if ragged else 7, lens=[7, 9, 3])
+    table, edges, slope = F.rand_bias(rng, H, nb, True)
+    far = int(c.pt[10])
+    points = c.points.copy()
+    points[0, far] = 1e30
+    c = F.Case(1, 30, 9, c.idx, c.n_valid, c.off, points, c.centers)
+    hit = c.pt == far
+    dbias = _features(rng, tuple(c.idx.shape) + (H,), dt)
+    flat = dbias.reshape(-1, H)
+    slots = torch.from_numpy(c.slot[hit])
+    flat[slots] = torch.tensor([INF, 2.0, -3.0, -INF, 0.0, NAN]).to(dt)
+    u, dist = c.places(edges)
+    dist[hit] = np.inf
+    g = flat.double().numpy()[c.slot]
+    with np.errstate(invalid="ignore"):
+        want_t, want_s = np.zeros((3, nb, H)), (g * dist[:, None]).sum(0)
+    for a in range(3):
+        np.add.at(want_t[a], u[:, a], g)
+    size = np.where(np.isfinite(g), np.abs(g), 0.0)
+    bound = len(g) * F.U * size.sum(0) + 1e-30
+    got = cagq.relative_bias_backward(c.groups(cagq, DEV), _bias((table, edges, slope)), dbias.to(DEV))
+    t = lambda x: torch.from_numpy(np.ascontiguousarray(x))  # noqa: E731
+    assert np.isnan(want_s[4:]).all() and np.array_equal(want_s[:4], [np.inf, np.inf, -np.inf, -np.inf])
+    F.check(dict(dtable=got[0], dslope=got[1]), dict(dtable=(t(want_t), t(np.broadcast_to(bound, want_t.shape))),
+                                                     dslope=(t(want_s), t(bound))), f"{dt} {ragged}")
