@@ -483,24 +483,31 @@ def _empty_as(like: torch.Tensor, stream):
     return _empty(like, like.shape, like.dtype, stream)
 
 
-def _handle(stream: Optional[torch.cuda.Stream]) -> int:
-    if stream is None and _raw_stream is not None and _cur_device is not None:
-        return _raw_stream(_cur_device())
-    return (stream or torch.cuda.current_stream()).cuda_stream
+def _handle(stream: Optional[torch.cuda.Stream], groups) -> int:
+    """The HIP stream to launch on; it and the groups have to be on the current device."""
+    cur = _cur_device() if _cur_device is not None else torch.cuda.current_device()
+    if cur != groups.index:
+        raise ValueError(f"groups on {groups.device}, but the current device is cuda:{cur}")
+    if stream is None:
+        return _raw_stream(cur) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+    if stream.device_index != cur:
+        raise ValueError(f"stream on cuda:{stream.device_index}, but the current device is cuda:{cur}")
+    return stream.cuda_stream
 
 
-def _with_workspace(call, size, workspace: Optional[torch.Tensor], like: torch.Tensor, stream, what: str):
-    """``call(address, bytes)`` with the workspace given, or one of the ``size(pointer)`` that the library asks for."""
+def _scratch(workspace: Optional[torch.Tensor], size, args, like: torch.Tensor, stream, what: str):
+    """Address and bytes of the workspace given, or of one as large as ``size(*args, pointer)`` says, and its tensor."""
     if workspace is None:
         need = C.c_size_t()
-        _check(size(C.byref(need)), what)
-        if need.value:
-            workspace = _empty(like, need.value, _U8, stream)
+        rc = size(*args, C.byref(need))
+        if rc:
+            raise CagqError(rc, what)
+        if not need.value:
+            return None, 0, None
+        workspace = _empty(like, need.value, _U8, stream)
     elif workspace.dtype is not _U8 or workspace.device != like.device or not workspace.is_contiguous():
         raise ValueError(f"workspace: expected contiguous torch.uint8 on {like.device}")
-    rc = call(None, 0) if workspace is None else call(workspace.data_ptr(), workspace.numel())
-    if rc:
-        raise CagqError(rc, what)
+    return workspace.data_ptr(), workspace.numel(), workspace
 
 
 class Groups:
@@ -510,7 +517,7 @@ class Groups:
     Fixed groups: ``idx`` int32 [B, M, K], of which the first ``n_valid`` int32 [B, M] slots count (all K where it
     is None). Ragged groups: ``off`` int64 [B*M + 1] and ``idx`` int32 [entries]. An index outside [0, N) is a
     masked slot. The tensors are borrowed and must live as long as the record is used."""
-    __slots__ = ("rec", "idx", "points", "centers", "n_valid", "off", "B", "N", "M", "K", "device")
+    __slots__ = ("rec", "idx", "points", "centers", "n_valid", "off", "B", "N", "M", "K", "device", "index")
 
     def __init__(self, idx: torch.Tensor, points: torch.Tensor, centers: torch.Tensor,
                  n_valid: Optional[torch.Tensor] = None, off: Optional[torch.Tensor] = None):
@@ -541,7 +548,7 @@ class Groups:
             _on(off, _I64, (B * M + 1,), "off", dev)
             of = off.data_ptr()
         self.idx, self.points, self.centers, self.n_valid, self.off = idx, points, centers, n_valid, off
-        self.B, self.N, self.M, self.K, self.device = B, N, M, K, dev
+        self.B, self.N, self.M, self.K, self.device, self.index = B, N, M, K, dev, cur
         self.rec = GroupsC(B, N, M, K, idx.data_ptr(), nv, of, entries, points.data_ptr(), centers.data_ptr())
 
     @property
@@ -619,6 +626,7 @@ def group_attention(groups: Groups, q: torch.Tensor, k: torch.Tensor, v: torch.T
     """Attention of each center over its group (cagq_group_attention): ``q`` [B, M, H, D], ``k`` and ``v``
     [B, N, Hkv, D] of float32, bfloat16 or float16. ``scale`` is D ** -0.5 by default; ``cap`` > 0 caps the scores
     by a tanh. Returns (out [B, M, H, D], lse float32 [B, M, H])."""
+    h = _handle(stream, groups)
     a = _attn(groups, q, k, v, bias, scale, cap)
     if out is None:
         out = _empty_as(q, stream)
@@ -629,10 +637,9 @@ def group_attention(groups: Groups, q: torch.Tensor, k: torch.Tensor, v: torch.T
     else:
         _on(lse, _F32, q.shape[:3], "lse", groups.device)
     L, g, ab, b = _lib or lib(), C.byref(groups.rec), C.byref(a), None if bias is None else C.byref(bias.rec)
-    _with_workspace(lambda p, n: L.cagq_group_attention(g, ab, b, q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                                        out.data_ptr(), lse.data_ptr(), p, n, _handle(stream)),
-                    lambda need: L.cagq_group_attention_workspace(g, ab, b, 0, need),
-                    workspace, q, stream, "cagq_group_attention")
+    p, n, _held = _scratch(workspace, L.cagq_group_attention_workspace, (g, ab, b, 0), q, stream, "cagq_group_attention")
+    _check(L.cagq_group_attention(g, ab, b, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
+                                  p, n, h), "cagq_group_attention")
     return out, lse
 
 
@@ -640,6 +647,7 @@ def point_lists(groups: Groups, off: Optional[torch.Tensor] = None, center: Opti
                 workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """The groups turned round (cagq_point_lists): offsets int64 [B*N + 1] and, for each point, the centers whose
     groups hold it, ascending, int32 [slots] (-1 behind the last list)."""
+    h = _handle(stream, groups)
     idx, points = groups.idx, groups.B * groups.N
     if off is None:
         off = _empty(idx, points + 1, _I64, stream)
@@ -650,9 +658,8 @@ def point_lists(groups: Groups, off: Optional[torch.Tensor] = None, center: Opti
     else:
         _on(center, _I32, center.shape, "center", groups.device)
     L, g = _lib or lib(), C.byref(groups.rec)
-    _with_workspace(lambda p, n: L.cagq_point_lists(g, off.data_ptr(), center.data_ptr(), center.numel(), p, n,
-                                                    _handle(stream)),
-                    lambda need: L.cagq_point_lists_workspace(g, need), workspace, idx, stream, "cagq_point_lists")
+    p, n, _held = _scratch(workspace, L.cagq_point_lists_workspace, (g,), idx, stream, "cagq_point_lists")
+    _check(L.cagq_point_lists(g, off.data_ptr(), center.data_ptr(), center.numel(), p, n, h), "cagq_point_lists")
     return off, center
 
 
@@ -664,6 +671,7 @@ def group_attention_backward(groups: Groups, lists, q: torch.Tensor, k: torch.Te
     """Gradients of ``group_attention`` for the gradient ``dout`` of its output (cagq_group_attention_backward),
     with ``lists`` from ``point_lists`` of the same groups: dq, dk, dv of the features' type, dtable and dslope
     float32 (None where the bias has no such part)."""
+    h = _handle(stream, groups)
     a = _attn(groups, q, k, v, bias, scale, cap)
     dev = groups.device
     off, center = lists
@@ -680,11 +688,12 @@ def group_attention_backward(groups: Groups, lists, q: torch.Tensor, k: torch.Te
         if bias.slope is not None:
             dslope = _empty_as(bias.slope, stream)
     L, g, ab = _lib or lib(), C.byref(groups.rec), C.byref(a)
-    _with_workspace(lambda p, n: L.cagq_group_attention_backward(
+    what = "cagq_group_attention_backward"
+    p, n, _held = _scratch(workspace, L.cagq_group_attention_workspace, (g, ab, b, 1), q, stream, what)
+    _check(L.cagq_group_attention_backward(
         g, ab, b, off.data_ptr(), center.data_ptr(), center.numel(), q.data_ptr(), k.data_ptr(), v.data_ptr(),
         lse.data_ptr(), dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(dtable), _ptr(dslope), p, n,
-        _handle(stream)), lambda need: L.cagq_group_attention_workspace(g, ab, b, 1, need),
-        workspace, q, stream, "cagq_group_attention_backward")
+        h), what)
     return dict(dq=dq, dk=dk, dv=dv, dtable=dtable, dslope=dslope)
 
 
@@ -692,6 +701,7 @@ def relative_bias(groups: Groups, bias: RelativeBias, dtype=torch.float32, out: 
                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """The relative position bias of every slot (cagq_relative_bias): [B, M, K, H], or [entries, H] of ragged
     groups; 0 in the slots that do not count."""
+    h = _handle(stream, groups)
     code = FEATURES.get(dtype)
     if code is None or bias.device != groups.device:
         raise ValueError(f"relative_bias: {dtype} with a bias on {bias.device} for groups on {groups.device}")
@@ -701,7 +711,7 @@ def relative_bias(groups: Groups, bias: RelativeBias, dtype=torch.float32, out: 
     else:
         _on(out, dtype, shape, "out", groups.device)
     _check((_lib or lib()).cagq_relative_bias(C.byref(groups.rec), C.byref(bias.rec), bias.H, code, out.data_ptr(),
-                                              _handle(stream)), "cagq_relative_bias")
+                                              h), "cagq_relative_bias")
     return out
 
 
@@ -710,7 +720,7 @@ def relative_bias_backward(groups: Groups, bias: RelativeBias, dbias: torch.Tens
                            stream: Optional[torch.cuda.Stream] = None):
     """(dtable, dslope), float32, for the gradient ``dbias`` of ``relative_bias``'s output
     (cagq_relative_bias_backward); None where the bias has no such part."""
-    dev = groups.device
+    dev, h = groups.device, _handle(stream, groups)
     code = FEATURES.get(dbias.dtype)
     if code is None or bias.device != dev:
         raise ValueError(f"relative_bias_backward: {dbias.dtype} with a bias on {bias.device} for groups on {dev}")
@@ -718,10 +728,9 @@ def relative_bias_backward(groups: Groups, bias: RelativeBias, dbias: torch.Tens
     dtable = None if bias.table is None else _empty_as(bias.table, stream)
     dslope = None if bias.slope is None else _empty_as(bias.slope, stream)
     L, g, b = _lib or lib(), C.byref(groups.rec), C.byref(bias.rec)
-    _with_workspace(lambda p, n: L.cagq_relative_bias_backward(g, b, bias.H, code, dbias.data_ptr(), _ptr(dtable),
-                                                               _ptr(dslope), p, n, _handle(stream)),
-                    lambda need: L.cagq_relative_bias_workspace(g, b, bias.H, need),
-                    workspace, dbias, stream, "cagq_relative_bias_backward")
+    what = "cagq_relative_bias_backward"
+    p, n, _held = _scratch(workspace, L.cagq_relative_bias_workspace, (g, b, bias.H), dbias, stream, what)
+    _check(L.cagq_relative_bias_backward(g, b, bias.H, code, dbias.data_ptr(), _ptr(dtable), _ptr(dslope), p, n, h), what)
     return dtable, dslope
 
 
