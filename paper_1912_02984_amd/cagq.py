@@ -516,7 +516,7 @@ class Groups:
 
     Fixed groups: ``idx`` int32 [B, M, K], of which the first ``n_valid`` int32 [B, M] slots count (all K where it
     is None). Ragged groups: ``off`` int64 [B*M + 1] and ``idx`` int32 [entries]. An index outside [0, N) is a
-    masked slot. The tensors are borrowed and must live as long as the record is used."""
+    masked slot. The record holds the tensors' addresses: they must keep their storage as long as it is used."""
     __slots__ = ("rec", "idx", "points", "centers", "n_valid", "off", "B", "N", "M", "K", "device", "index")
 
     def __init__(self, idx: torch.Tensor, points: torch.Tensor, centers: torch.Tensor,
@@ -559,11 +559,17 @@ class Groups:
 class RelativeBias:
     """Relative position bias of H heads: ``table`` [3, buckets, H] read by the buckets that the ascending
     ``edges`` [3, buckets - 1] cut each axis into, and ``slope`` [H] times the distance (float32; either may be
-    None). The tensors are borrowed."""
-    __slots__ = ("rec", "table", "edges", "slope", "H", "device")
+    None). What is learned may be given other storage (``table.data = ...``, a module's ``.to``): each call reads
+    what ``table`` and ``slope`` hold by then, after the checks made here. ``edges`` must keep theirs."""
+    __slots__ = ("rec", "table", "edges", "slope", "H", "device", "table_at", "slope_at")
 
     def __init__(self, table: Optional[torch.Tensor] = None, edges: Optional[torch.Tensor] = None,
                  slope: Optional[torch.Tensor] = None):
+        self.table, self.edges, self.slope = table, edges, slope
+        self._make()
+
+    def _make(self):
+        table, edges, slope = self.table, self.edges, self.slope
         some = table if table is not None else slope
         if some is None or not some.is_cuda:
             raise ValueError("a bias needs a table or a slope, on the GPU")
@@ -583,8 +589,15 @@ class RelativeBias:
         if slope is not None:
             _on(slope, _F32, (H,), "slope", dev)
             sp = slope.data_ptr()
-        self.table, self.edges, self.slope, self.H, self.device = table, edges, slope, H, dev
+        self.H, self.device, self.table_at, self.slope_at = H, dev, tp, sp
         self.rec = BiasC(tp, ep, sp, nb)
+
+    def ref(self):
+        """The C record, by reference."""
+        t, s = self.table, self.slope
+        if (t is not None and t.data_ptr() != self.table_at) or (s is not None and s.data_ptr() != self.slope_at):
+            self._make()
+        return C.byref(self.rec)
 
 
 def _row(t: torch.Tensor, name: str) -> int:
@@ -626,7 +639,7 @@ def group_attention(groups: Groups, q: torch.Tensor, k: torch.Tensor, v: torch.T
     """Attention of each center over its group (cagq_group_attention): ``q`` [B, M, H, D], ``k`` and ``v``
     [B, N, Hkv, D] of float32, bfloat16 or float16. ``scale`` is D ** -0.5 by default; ``cap`` > 0 caps the scores
     by a tanh. Returns (out [B, M, H, D], lse float32 [B, M, H])."""
-    h = _handle(stream, groups)
+    h, b = _handle(stream, groups), None if bias is None else bias.ref()
     a = _attn(groups, q, k, v, bias, scale, cap)
     if out is None:
         out = _empty_as(q, stream)
@@ -636,7 +649,7 @@ def group_attention(groups: Groups, q: torch.Tensor, k: torch.Tensor, v: torch.T
         lse = _empty(q, q.shape[:3], _F32, stream)
     else:
         _on(lse, _F32, q.shape[:3], "lse", groups.device)
-    L, g, ab, b = _lib or lib(), C.byref(groups.rec), C.byref(a), None if bias is None else C.byref(bias.rec)
+    L, g, ab = _lib or lib(), C.byref(groups.rec), C.byref(a)
     p, n, _held = _scratch(workspace, L.cagq_group_attention_workspace, (g, ab, b, 0), q, stream, "cagq_group_attention")
     _check(L.cagq_group_attention(g, ab, b, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr(),
                                   p, n, h), "cagq_group_attention")
@@ -671,7 +684,7 @@ def group_attention_backward(groups: Groups, lists, q: torch.Tensor, k: torch.Te
     """Gradients of ``group_attention`` for the gradient ``dout`` of its output (cagq_group_attention_backward),
     with ``lists`` from ``point_lists`` of the same groups: dq, dk, dv of the features' type, dtable and dslope
     float32 (None where the bias has no such part)."""
-    h = _handle(stream, groups)
+    h, b = _handle(stream, groups), None if bias is None else bias.ref()
     a = _attn(groups, q, k, v, bias, scale, cap)
     dev = groups.device
     off, center = lists
@@ -680,9 +693,8 @@ def group_attention_backward(groups: Groups, lists, q: torch.Tensor, k: torch.Te
     _on(lse, _F32, q.shape[:3], "lse", dev)
     _on(dout, q.dtype, q.shape, "dout", dev)
     dq, dk, dv = _empty_as(dout, stream), _empty_as(k, stream), _empty_as(k, stream)
-    dtable = dslope = b = None
+    dtable = dslope = None
     if bias is not None:
-        b = C.byref(bias.rec)
         if bias.table is not None:
             dtable = _empty_as(bias.table, stream)
         if bias.slope is not None:
@@ -701,7 +713,7 @@ def relative_bias(groups: Groups, bias: RelativeBias, dtype=torch.float32, out: 
                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """The relative position bias of every slot (cagq_relative_bias): [B, M, K, H], or [entries, H] of ragged
     groups; 0 in the slots that do not count."""
-    h = _handle(stream, groups)
+    h, b = _handle(stream, groups), bias.ref()
     code = FEATURES.get(dtype)
     if code is None or bias.device != groups.device:
         raise ValueError(f"relative_bias: {dtype} with a bias on {bias.device} for groups on {groups.device}")
@@ -710,7 +722,7 @@ def relative_bias(groups: Groups, bias: RelativeBias, dtype=torch.float32, out: 
         out = _empty(groups.idx, shape, dtype, stream)
     else:
         _on(out, dtype, shape, "out", groups.device)
-    _check((_lib or lib()).cagq_relative_bias(C.byref(groups.rec), C.byref(bias.rec), bias.H, code, out.data_ptr(),
+    _check((_lib or lib()).cagq_relative_bias(C.byref(groups.rec), b, bias.H, code, out.data_ptr(),
                                               h), "cagq_relative_bias")
     return out
 
@@ -720,14 +732,14 @@ def relative_bias_backward(groups: Groups, bias: RelativeBias, dbias: torch.Tens
                            stream: Optional[torch.cuda.Stream] = None):
     """(dtable, dslope), float32, for the gradient ``dbias`` of ``relative_bias``'s output
     (cagq_relative_bias_backward); None where the bias has no such part."""
-    dev, h = groups.device, _handle(stream, groups)
+    dev, h, b = groups.device, _handle(stream, groups), bias.ref()
     code = FEATURES.get(dbias.dtype)
     if code is None or bias.device != dev:
         raise ValueError(f"relative_bias_backward: {dbias.dtype} with a bias on {bias.device} for groups on {dev}")
     _on(dbias, dbias.dtype, (*groups.idx.shape, bias.H), "dbias", dev)
     dtable = None if bias.table is None else _empty_as(bias.table, stream)
     dslope = None if bias.slope is None else _empty_as(bias.slope, stream)
-    L, g, b = _lib or lib(), C.byref(groups.rec), C.byref(bias.rec)
+    L, g = _lib or lib(), C.byref(groups.rec)
     what = "cagq_relative_bias_backward"
     p, n, _held = _scratch(workspace, L.cagq_relative_bias_workspace, (g, b, bias.H), dbias, stream, what)
     _check(L.cagq_relative_bias_backward(g, b, bias.H, code, dbias.data_ptr(), _ptr(dtable), _ptr(dslope), p, n, h), what)

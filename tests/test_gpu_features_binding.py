@@ -50,3 +50,40 @@ def test_streams_of_another_device_are_refused():
     for f in _calls(_made()):
         with pytest.raises(ValueError, match="stream"):
             f(SimpleNamespace(cuda_stream=0, device_index=1, device=torch.device("cuda:1")))
+
+
+def test_a_bias_follows_what_is_learned():
+    """A learned table and slope that are given other storage after the record was made: the calls read what they
+    hold now (the old storage is kept here), and refuse what no longer fits."""
+    m = _made(2)
+    keep, calls = [], _calls(m)
+
+    def flat(x):
+        x = list(x.values()) if isinstance(x, dict) else [x] if torch.is_tensor(x) else list(x)
+        return [t for t in x if t is not None]
+
+    def swap(t, value):
+        keep.append(t.data)
+        t.data = value
+
+    b = m.b
+    first = flat(calls[0](None))
+    for t, value in ((b.table, b.table * 2 + 1), (b.slope, b.slope - 1)):
+        swap(t, value)
+        m.b = cagq.RelativeBias(b.table.clone(), b.edges, b.slope.clone())
+        want = [flat(f(None)) for f in _calls(m)]
+        m.b = b
+        got = [flat(f(None)) for f in _calls(m)]
+        for x, y in zip(got, want):
+            assert len(x) == len(y) and all(torch.equal(s, t) for s, t in zip(x, y))
+    assert not torch.equal(got[0][0], first[0])
+    calls = _calls(m)
+    del calls[1]  # the lists take no bias
+    for t, value in ((b.table, b.table[:, :, :1].contiguous()), (b.table, b.table.cpu()), (b.slope, b.slope.repeat(2))):
+        old = t.data
+        swap(t, value)
+        for f in calls:
+            with pytest.raises(ValueError):
+                f(None)
+        t.data = old
+        calls[0](None)
