@@ -221,6 +221,14 @@ struct Score : PlaceBias {
 
 // exp(x) of a difference of scores.
 __device__ __forceinline__ float weight(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ __forceinline__ float weight(float x, float log2_part) {
+    return __builtin_amdgcn_exp2f(fmaf(x, kLog2e, log2_part));
+}
+
+// Of a row and head, from the gradient at the centers to the one at the points.
+struct Stat {
+    float z, delta, log_part;  // lse (infinity: none), sum p dp, log2 of what the weights are multiplied by
+};
 
 // log of a sum of weights.
 __device__ __forceinline__ float log_sum(float x) { return kLn2 * __builtin_amdgcn_logf(x); }
@@ -625,13 +633,11 @@ __global__ __launch_bounds__(kAtThreads) void k_at_join(Partial part, int64_t ro
 // the list, in fp32. The weights' sum is 1 but for the rounding of lse, which
 // all of a list share; dividing delta by it keeps the sum of a list's ds at 0,
 // on which the sums over many lists in the bias's gradient rely.
-// stat: (lse, delta) of each row and head, for the points; share: what their
-// weights are multiplied by, of groups above kFarLse alone.
+// stat: what the points need of each row and head.
 template <typename T, bool BUF, bool EACH>
 __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn a, Lanes l, Walk walk,
                                                           const float* __restrict__ lse, const T* __restrict__ dout,
-                                                          T* __restrict__ dq, float2* __restrict__ stat,
-                                                          float* __restrict__ share) {
+                                                          T* __restrict__ dq, Stat* __restrict__ stat) {
     constexpr int W = kVec<T>;
     constexpr int U = kUnroll<1>;
     extern __shared__ __align__(16) float s_lds[];
@@ -748,10 +754,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
 #pragma unroll
         for (int w = 0; w < W; ++w) acc[w] = a.scale * part * fmaf(-delta, acd[w], acc[w]);
         store_channels<T, BUF>(dq + rh * a.D + at.chan, at.n, acc);
-        if (at.chan == 0) {
-            stat[rh] = make_float2(z, delta);
-            if (far) share[rh] = part;
-        }
+        if (at.chan == 0) stat[rh] = Stat{z, delta, far ? __builtin_amdgcn_logf(part) : 0.0f};
     });
 }
 
@@ -768,8 +771,7 @@ template <typename T, bool BUF, bool FLAT, bool TAB>
 __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn a, Lanes l, Walk walk,
                                                           const int64_t* __restrict__ pt_off,
                                                           const int32_t* __restrict__ pt_center, int64_t capacity,
-                                                          const float2* __restrict__ stat,
-                                                          const float* __restrict__ share, const T* __restrict__ dout,
+                                                          const Stat* __restrict__ stat, const T* __restrict__ dout,
                                                           T* __restrict__ dk, T* __restrict__ dv,
                                                           float* __restrict__ part) {
     constexpr int W = kVec<T>;
@@ -816,8 +818,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
         const int64_t kd = (int64_t)a.Hkv * a.D;
         const RowsOut<T, BUF> dkr(dk + p0 * kd, kd, at.head * a.D + at.chan, at.n);
         const RowsOut<T, BUF> dvr(dv + p0 * kd, kd, at.head * a.D + at.chan, at.n);
-        const float2* st0 = stat + c0 * a.H;
-        const float* share0 = share + c0 * a.H;
+        const Stat* st0 = stat + c0 * a.H;
         auto clip = [&](int64_t x) { return x < 0 ? 0 : x > capacity ? capacity : x; };
         const int64_t beg = clip(pt_off[p0 + i0]);
         int64_t total = clip(pt_off[p0 + i0 + n0]) - beg;
@@ -901,7 +902,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                 }
                 Raw q[U], go[U], kx[U], vx[U];
                 float s[2 * U], bi[U], pd[U];
-                float2 st[U];
+                Stat st[U];
                 uint32_t pu[U];
                 int32_t pk[U];
                 bool there[U];
@@ -939,14 +940,9 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
                     float dp = s[2 * i + 1];
-                    float v = s[2 * i] + bi[i], part = 1.0f;
-                    if (__any(bi[i] == kNegInf || fabsf(st[i].x) > kFarLse)) {
+                    float v = s[2 * i] + bi[i];
+                    if (__any(bi[i] == kNegInf)) {
                         rare();
-                        if (there[i] && fabsf(st[i].x) > kFarLse) {
-                            const float* r0 = ck.row(at_row[i]);
-                            const int64_t c = BUF ? (int64_t)ck.field(r0, kStat) : (int64_t)ck.field(r0, kKey) * a.H;
-                            part = share0[c + at.head * Rq + rr[i]];
-                        }
                         if (bi[i] == kNegInf) {
                             q[i] = go[i] = Raw{0, 0, 0, 0};
                             v = kNegInf;
@@ -955,8 +951,8 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                             pd[i] = 0.0f;  // a distance that overflows, under a negative slope
                         }
                     }
-                    const float p = there[i] ? weight(v - st[i].x) * part : 0.0f;
-                    const float ds = there[i] ? p * (dp - st[i].y) : 0.0f;
+                    const float p = there[i] ? weight(v - st[i].z, st[i].log_part) : 0.0f;
+                    const float ds = there[i] ? p * (dp - st[i].delta) : 0.0f;
                     const float da = there[i] ? ds * Score::slack(e2[i]) : 0.0f;
                     if (FLAT) {
                         const bool change = pk[i] >= 0 && pk[i] != cur;
@@ -1014,8 +1010,7 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
 
 // ------------------------------------------------------------------ host side
 
-// What the centers' pass of the gradients leaves for the points': (lse, delta) and a share for each row and head.
-size_t stat_bytes(int64_t rh) { return ((size_t)rh * 12 + 255) & ~(size_t)255; }
+size_t stat_bytes(int64_t rh) { return ((size_t)rh * sizeof(Stat) + 255) & ~(size_t)255; }
 
 // Whether every slot of a wave takes a list of its own: lists short, and the
 // shorter the fewer of them that takes. (Mean lengths of 5 and 8, 5870 and 4542
@@ -1147,14 +1142,14 @@ hipError_t forward(const Groups& g, int32_t B, const Attn& a, const Bias& b, voi
 
 template <typename T, bool BUF, bool EACH>
 hipError_t back_centers(const Groups& g, int32_t B, const Attn& a, const Bias& b, const Lanes& l, const float* lse,
-                        const void* dout, void* dq, float2* stat, float* share, hipStream_t s) {
+                        const void* dout, void* dq, Stat* stat, hipStream_t s) {
     const Walk w = make_walk(B, g.M, EACH ? l.S : 1, 1);
     const Shape sh = shape_of(b, Chunk::floats(placed(b), Rounds<EACH, kUnroll<1>>::rows_n(l), l.Hc));
     auto kern = k_at_back_c<T, BUF, EACH>;
     hipError_t e = allow_lds(kern, sh.lds);
     if (e != hipSuccess) return e;
     kern<<<dim3(blocks_of(w.units, sh.waves, EACH ? kAtBlocks : kAtMany), l.passes), sh.waves * kWave, sh.lds, s>>>(
-        g, b, a, l, w, lse, (const T*)dout, (T*)dq, stat, share);
+        g, b, a, l, w, lse, (const T*)dout, (T*)dq, stat);
     return hipGetLastError();
 }
 
@@ -1213,8 +1208,7 @@ hipError_t backward(const Groups& g, int32_t B, const Attn& a, const Bias& b, co
                     void* dv, float* dtable, float* dslope, void* ws, hipStream_t s) {
     const Lanes lc = make_lanes<T>(a.H, a.D);
     const int64_t rh = (int64_t)g.rows * a.H;
-    float2* stat = (float2*)ws;
-    float* share = (float*)(stat + rh);
+    Stat* stat = (Stat*)ws;
     float* part = (float*)((char*)ws + stat_bytes(rh));
     const bool buf = vectors<T>(g, a, {a.q, a.k, a.v, dout, dq, dk, dv});
     const bool ec = each_of(g.rows, g.idx_len, lc), tab = dtable || dslope;
@@ -1225,10 +1219,10 @@ hipError_t backward(const Groups& g, int32_t B, const Attn& a, const Bias& b, co
     if (e != hipSuccess) return e;
     auto centers = buf ? (ec ? back_centers<T, true, true> : back_centers<T, true, false>)
                        : (ec ? back_centers<T, false, true> : back_centers<T, false, false>);
-    e = centers(g, B, a, b, lc, lse, dout, dq, stat, share, s);
+    e = centers(g, B, a, b, lc, lse, dout, dq, stat, s);
     if (e != hipSuccess) return e;
     points<<<dim3(r.blocks, r.l.passes), r.sh.waves * kWave, r.sh.lds, s>>>(
-        g, b, a, r.l, r.walk, pt_off, pt_center, capacity, stat, share, (const T*)dout, (T*)dk, (T*)dv, part);
+        g, b, a, r.l, r.walk, pt_off, pt_center, capacity, stat, (const T*)dout, (T*)dk, (T*)dv, part);
     e = hipGetLastError();
     if (e != hipSuccess || !tab) return e;
     return launch_bias_reduce(part, (int32_t)r.blocks, b, dtable, dslope, s);
