@@ -625,7 +625,7 @@ def _attn(groups: Groups, q, k, v, bias: Optional[RelativeBias], scale, cap):
                              f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     _, _, H, D = q.shape
     _, _, Hkv, Dk = k.shape
-    if v.shape != k.shape or Dk != D or Hkv < 1 or H % Hkv:
+    if v.shape != k.shape or Dk != D or D < 1 or Hkv < 1 or H % Hkv:
         raise ValueError(f"heads of q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not fit")
     if bias is not None and (bias.H != H or bias.device != dev):
         raise ValueError(f"bias: expected {H} heads on {dev}, got {bias.H} on {bias.device}")

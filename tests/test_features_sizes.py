@@ -1,7 +1,9 @@
 """Sizes that the operators on point features ask for, over the stated limits, without a GPU."""
 import ctypes as C
+from types import SimpleNamespace
 
 import pytest
+import torch
 
 from paper_1912_02984_amd import cagq
 
@@ -28,3 +30,12 @@ def test_workspace_of_a_bias_gradient(dtype, H, Hkv, D, nb):
         got = _workspace(g, a, b, 1)
         assert least < got <= most + BLOCKS * (3 * nb + 1) * H * 4
         assert (got - least) >= 4 * (3 * nb + 1) * H
+
+
+@pytest.mark.parametrize("H,Hkv,D", [(2, 2, 0), (2, 0, 8), (0, 0, 0)])
+def test_rows_of_nothing_are_refused(H, Hkv, D):
+    """By the binding, as heads that do not fit: before a scale is made of the width."""
+    groups = SimpleNamespace(B=1, N=5, M=3, device=torch.device("cpu"))
+    q, k = torch.zeros(1, 3, H, D), torch.zeros(1, 5, Hkv, D)
+    with pytest.raises(ValueError, match="heads"):
+        cagq._attn(groups, q, k, k, None, None, 0.0)
