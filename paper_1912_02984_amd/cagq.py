@@ -638,7 +638,8 @@ def group_attention(groups: Groups, q: torch.Tensor, k: torch.Tensor, v: torch.T
                     workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """Attention of each center over its group (cagq_group_attention): ``q`` [B, M, H, D], ``k`` and ``v``
     [B, N, Hkv, D] of float32, bfloat16 or float16. ``scale`` is D ** -0.5 by default; ``cap`` > 0 caps the scores
-    by a tanh. Returns (out [B, M, H, D], lse float32 [B, M, H])."""
+    by a tanh. Returns (out [B, M, H, D], lse float32 [B, M, H]), which carry no autograd graph, whatever the inputs
+    require: ``group_attention_backward`` makes the gradients."""
     h, b = _handle(stream, groups), None if bias is None else bias.ref()
     a = _attn(groups, q, k, v, bias, scale, cap)
     if out is None:
@@ -683,7 +684,7 @@ def group_attention_backward(groups: Groups, lists, q: torch.Tensor, k: torch.Te
                              stream: Optional[torch.cuda.Stream] = None) -> Dict[str, Optional[torch.Tensor]]:
     """Gradients of ``group_attention`` for the gradient ``dout`` of its output (cagq_group_attention_backward),
     with ``lists`` from ``point_lists`` of the same groups: dq, dk, dv of the features' type, dtable and dslope
-    float32 (None where the bias has no such part)."""
+    float32 (None where the bias has no such part). ``dout`` and ``lse`` must be contiguous."""
     h, b = _handle(stream, groups), None if bias is None else bias.ref()
     a = _attn(groups, q, k, v, bias, scale, cap)
     dev = groups.device
@@ -712,7 +713,8 @@ def group_attention_backward(groups: Groups, lists, q: torch.Tensor, k: torch.Te
 def relative_bias(groups: Groups, bias: RelativeBias, dtype=torch.float32, out: Optional[torch.Tensor] = None,
                   stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """The relative position bias of every slot (cagq_relative_bias): [B, M, K, H], or [entries, H] of ragged
-    groups; 0 in the slots that do not count."""
+    groups; 0 in the slots that do not count. It carries no autograd graph: ``relative_bias_backward`` makes the
+    gradients."""
     h, b = _handle(stream, groups), bias.ref()
     code = FEATURES.get(dtype)
     if code is None or bias.device != groups.device:

@@ -13,9 +13,11 @@
 //   - two to four rows of each slot are loaded before the first is used. Loads go
 //     through a bounds-checked buffer, in which an entry that is not there has
 //     an offset past the end and reads as zeros, without a branch;
-//   - two ways to share a wave: EACH, a list per slot (many short lists: no
-//     slot waits for another list's end, nothing is joined), or one list for
-//     all slots, joined by permutes at its end.
+//   - three ways to share the work: EACH, a list per slot (many short lists: no
+//     slot waits for another list's end, nothing is joined); one list for all of
+//     a wave's slots, joined by permutes at its end; BLOCK, in the forward pass
+//     alone, one list for all of a workgroup's waves, joined in LDS, in parts
+//     where lists are few.
 // Scores stay in natural units (times log2 e, a bias of the type's lowest
 // value would become -infinity), and only differences of them are taken to
 // base 2.
@@ -23,12 +25,14 @@
 // The gradients take two passes: at the centers (dq, and delta = sum p dp) and
 // at the points (dk, dv and the bias's), each recomputing the scores: that
 // reads two rows a pair, as storing and fetching weights for every pair and
-// head would need memory for them all.
+// head would need memory for them all. An entry that is not there, and a pair
+// that the bias masks, add zeros to every sum whatever k, v, q and dout hold: a
+// value that is not finite is selected away, not multiplied by 0.
 //
 // Measured on indoor scenes (4 x 81920 points, 8192 centers of 32, 8 heads of
 // 32 channels in bfloat16: 779000 pairs, of which each reads two rows of 512
-// bytes): forward 100 us, gradients 112 us at the centers and 250 us at the
-// points. The caches' misses bound all three: 0.58, 0.60 and 1.29 GB at 5.1 to
+// bytes): forward 100 us, gradients 113 us at the centers and 257 us at the
+// points. The caches' misses bound all three: 0.58, 0.60 and 1.32 GB at 5.1 to
 // 5.8 TB/s (rows are as much as a cloud's 84 MB apart in time of use, an L2
 // holds 4 MB), against 0.35 GB that the forward cannot do without; its loads
 // without any arithmetic take 97 us. Short rows are bound by issue instead:

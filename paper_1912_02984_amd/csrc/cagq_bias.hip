@@ -1,9 +1,10 @@
 // The relative position bias alone, and its gradient (cagq_relative_bias,
 // cagq_relative_bias_backward; the definition is in include/cagq.h).
 // Indoor scenes (2^20 slots, 8 heads in bfloat16): 17 us for the bias, of which
-// 16.8 MB of stores and 13 MB of reads would take 6 at the card's copy rate: a
-// lane's searches in the edges and its three table rows in LDS are the rest. The
-// gradient takes 43 us and the sum over its workgroups' tables 7.
+// 16.8 MB of stores and 13 MB of reads would take 6 at the card's copy rate. It
+// reads 37 MB past the L2, which with the stores makes 11 of it; a lane's searches
+// in the edges and its three table rows in LDS are the rest. The gradient takes 44
+// us and the sum over its workgroups' tables 7.
 #include "cagq_features.h"
 
 namespace cagq {
