@@ -720,15 +720,12 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_c(Groups g, Bias b, Attn
                 sc.template products<T, U, 2>(s, e2);
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
-                    float dp = s[2 * i + 1];
-                    float x = s[2 * i] + bi[i];
+                    const float dp = s[2 * i + 1], x = s[2 * i] + bi[i];
                     if (__any(bi[i] == kNegInf)) {  // masked by the bias: whatever k and v hold
                         rare();
                         if (bi[i] == kNegInf) {
                             k[i] = Raw{0, 0, 0, 0};
-                            x = kNegInf;
-                            dp = 0.0f;
-                            e2[i] = 0.5f;
+                            there[i] = false;
                         }
                     }
                     // an entry that is not there: its zeros times a q or dout that is not finite are none
@@ -943,16 +940,12 @@ __global__ __launch_bounds__(kAtThreads) void k_at_back_p(Groups g, Bias b, Attn
                 sc.template products<T, U, 2>(s, e2);
 #pragma unroll
                 for (int i = 0; i < U; ++i) {
-                    float dp = s[2 * i + 1];
-                    float v = s[2 * i] + bi[i];
+                    const float dp = s[2 * i + 1], v = s[2 * i] + bi[i];
                     if (__any(bi[i] == kNegInf)) {
                         rare();
                         if (bi[i] == kNegInf) {
                             q[i] = go[i] = Raw{0, 0, 0, 0};
-                            v = kNegInf;
-                            dp = 0.0f;
-                            e2[i] = 0.5f;
-                            pd[i] = 0.0f;  // a distance that overflows, under a negative slope
+                            there[i] = false;  // nor lse, delta and a distance that overflows
                         }
                     }
                     const float p = there[i] ? weight(v - st[i].z, st[i].log_part) : 0.0f;

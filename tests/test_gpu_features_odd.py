@@ -229,3 +229,26 @@ def test_relative_bias_gradient_at_a_distance_that_overflows(dt, ragged):
     assert np.isnan(want_s[4:]).all() and np.array_equal(want_s[:4], [np.inf, np.inf, -np.inf, -np.inf])
     F.check(dict(dtable=got[0], dslope=got[1]), dict(dtable=(t(want_t), t(np.broadcast_to(bound, want_t.shape))),
                                                      dslope=(t(want_s), t(bound))), f"{dt} {ragged}")
+
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("cap", [0.0, 9.0])
+@pytest.mark.parametrize("way", range(len(WAYS)))
+def test_masked_points_of_groups_that_are_not_finite(dt, cap, way):
+    """Groups whose q or dout is not finite, and whose gradients are not: the points that the bias masks in them get
+    zeros all the same, and so does the bucket that no other pair is in."""
+    rng = np.random.default_rng(251 + way)
+    c = _groups(rng, **WAYS[way])
+    c.points[:, ::3, 0] -= 100.0
+    H, Hkv, D = 4, 2, 16
+    q, k, v, dout = (_features(rng, (2, n, h, D), dt) for n, h in ((c.M, H), (c.N, Hkv), (c.N, Hkv), (c.M, H)))
+    rows = rng.random((2, c.M)) < 0.5
+    rows[:, 0] = True
+    odd = torch.from_numpy(rows)[..., None].expand(2, c.M, H)
+    table, edges, slope = F.rand_bias(rng, H, 6, True)
+    edges[:, 0] = -50.0
+    table[0, 0] = -np.inf
+    for x in ((_odd(q, odd), dout), (q, _odd(dout, odd))):
+        got = _attend(c, x[0], k, v, (table, edges, slope), None, cap, x[1])
+        assert not torch.isfinite(got["dk"]).all()
+        assert (got["dk"][:, ::3] == 0).all() and (got["dv"][:, ::3] == 0).all() and (got["dtable"][0, 0] == 0).all()
